@@ -81,7 +81,7 @@ enum { EP_ORDER_TOKEN = 0, EP_ORDER_DESTINATION = 1, EP_ORDER_DESTINATION_RESIDE
 enum { EP_DTYPE_BF16 = 0, EP_DTYPE_F32 = 1, EP_DTYPE_I32 = 2, EP_DTYPE_U8 = 3,
        EP_DTYPE_FP8_E4M3 = 4 /* OCP E4M3: 1-4-3 bits, bias 7, max 448, no infinity */ };
 
-/* Tensor roles (Sec. III-E, Table IV).  The last three are this library's own. */
+/* Tensor roles (Sec. III-E, Table IV).  The last ones, from RECV_SRC_TOKEN on, are this library's own. */
 enum {
     EP_TAG_NONE = 0,
     EP_TAG_TOKENS = 1,                     /* token data, input or output                 */
@@ -93,9 +93,27 @@ enum {
     EP_TAG_TOKENS_PER_EXPERTS = 7,         /* same as RECV_EXPERT_COUNTER_DEVICE          */
     EP_TAG_RECV_SRC_TOKEN = 8,             /* int32 [rows] source token index of each row */
     EP_TAG_EXPERT_BASE = 9,                /* int32 [E], see ep_layout                    */
-    EP_TAG_EXPERT_TOKENS = 10              /* expert outputs, shaped like dispatch's TOKENS
+    EP_TAG_EXPERT_TOKENS = 10,             /* expert outputs, shaped like dispatch's TOKENS
                                               output (input of ep_combine_backward)       */
+    /* the gate, the experts' products and the layer of few tokens */
+    EP_TAG_LOGITS = 11,                    /* gate logits [T, E] and their gradient       */
+    EP_TAG_SELECT_BIAS = 12,               /* f32 [E] added to the scores for selecting   */
+    EP_TAG_EXPERT_WEIGHTS = 13,            /* bf16 [L, N, Kd] and their gradient          */
+    EP_TAG_EXPERT_BIAS = 14,               /* [L, N] and its gradient                     */
+    EP_TAG_RESIDUAL = 15,                  /* bf16 rows added to the output               */
+    EP_TAG_PREACT = 16,                    /* bf16 rows before the activation, and their gradient */
+    EP_TAG_ROW_OFFSET = 17,                /* int32 [L] first row of each expert          */
+    EP_TAG_ROW_COUNT = 18,                 /* int32 [L] rows of each expert               */
+    EP_TAG_DOWN_WEIGHTS = 19,              /* bf16 [L, H, I] second product of a layer    */
+    EP_TAG_DOWN_BIAS = 20,                 /* [L, H]                                      */
+    EP_TAG_WORKSPACE = 21                  /* u8 [bytes], see ep_expert_layer_plan        */
 };
+
+/* Gate scores: softmax over the experts of a token, or the sigmoid of each logit. */
+enum { EP_SCORE_SOFTMAX = 0, EP_SCORE_SIGMOID = 1 };
+
+/* Activations of the experts' products: silu(v) = v / (1 + exp(-v)), gelu(v) = v (1 + erf(v / sqrt 2)) / 2. */
+enum { EP_ACT_NONE = 0, EP_ACT_SILU = 1, EP_ACT_GELU = 2 };
 
 /* N-d tensor descriptor (Sec. III-E): shape and strides in ELEMENTS, innermost
  * stride must be 1; rows of bf16 token tensors must start on 16-byte boundaries
@@ -570,6 +588,133 @@ EP_API ep_result_t ep_complete(ep_handle_t handle, const ep_complete_config_t *c
 
 /* Clears every coordination counter of the group (e.g. after an abandoned staged call). */
 EP_API ep_result_t ep_group_reset_signals(ep_group_t group, ep_stream_t stream);
+
+/*
+ * The gate, the experts' products and the layer of few tokens: what a program computes around
+ * layout, dispatch and combine.  They keep no state between calls and allocate nothing; everything is
+ * enqueued on `stream`, so calls can be captured into a graph.  No output may share memory with an
+ * input unless a comment says so.
+ */
+
+/* Rule of the gate.  `size` must be sizeof(ep_route_config_t). */
+typedef struct {
+    uint32_t size;
+    int32_t score;        /* EP_SCORE_SOFTMAX / EP_SCORE_SIGMOID                                     */
+    int32_t renormalise;  /* 1: the weights of a token are divided by their sum                      */
+    int32_t num_groups;   /* experts form this many equal, consecutive groups (1 = no groups, <= 64) */
+    int32_t groups_kept;  /* and are chosen from the best groups_kept of them                        */
+    float scale;          /* factor of all weights (finite)                                          */
+} ep_route_config_t;
+
+/*
+ * ep_route -- the gate: the K experts of each token and their weights, as ep_layout, ep_dispatch and
+ * ep_combine take them.
+ * inputs:  LOGITS l [T, E] f32 or bf16, any row stride (E <= 1024); SELECT_BIAS b f32 [E] (optional).
+ * outputs: TOPK_IDX int32 [T, K] (K <= 64); TOPK_WEIGHTS f32 [T, K].
+ * s = softmax(l) over the token's routable experts, or sigmoid(l).  An expert is not routable where its
+ * logit is -inf or NaN (or its bias is); +inf counts as the largest finite float.  The K routable experts
+ * with the largest s + b are taken in descending order, ties to the lower id; with groups only experts of
+ * the groups_kept groups with the largest sum of their two largest s + b (of the one routable member, if
+ * there are no two; ties to the lower group).  Without bias and groups the order is that of the logits,
+ * exactly; otherwise s + b is computed in 64 bits.  b takes part in the choice only:
+ *     w[t,k] = scale * s[idx[t,k]] / (renormalise ? sum over the token's idx of s : 1)
+ * in float32.  Entries that no routable expert is left for get id -1 and weight 0.
+ * Errors: EP_ERR_INVALID_ARG, EP_ERR_HIP.
+ */
+EP_API ep_result_t ep_route(const ep_route_config_t *cfg, const ep_tensor_t *inputs, int32_t num_inputs,
+                            const ep_tensor_t *outputs, int32_t num_outputs, ep_stream_t stream);
+
+/*
+ * ep_route_backward -- gradient of the logits from that of the weights, the choice of experts being fixed.
+ * inputs:  LOGITS l [T, E] as given to ep_route; TOPK_IDX [T, K] as it returned them (ids outside [0, E)
+ *          have no gradient; an id may come twice in a token); TOPK_WEIGHTS g f32 [T, K]: gradient of the weights.
+ * outputs: LOGITS [T, E] of the type of l: every element is written.
+ * The groups of cfg play no part.  Errors: EP_ERR_INVALID_ARG, EP_ERR_HIP.
+ */
+EP_API ep_result_t ep_route_backward(const ep_route_config_t *cfg, const ep_tensor_t *inputs, int32_t num_inputs,
+                                     const ep_tensor_t *outputs, int32_t num_outputs, ep_stream_t stream);
+
+/* Options of the experts' products and of the layer.  `size` must be sizeof(ep_product_config_t). */
+typedef struct {
+    uint32_t size;
+    int32_t activation;   /* EP_ACT_*                                                                 */
+    int32_t gated;        /* 1: of the N weight rows the first half is the gate, the second the up
+                             projection, and act(gate) * up has N/2 elements                          */
+    int32_t first_expert; /* expert of the handle (of the ids, for the layer) that the first of the
+                             weights belongs to: a program that owns some of the experts passes their
+                             weights only                                                             */
+    int32_t accumulate;   /* ep_expert_product_backward: gradients of weights and bias are added to
+                             what their tensors hold                                                  */
+} ep_product_config_t;
+
+/*
+ * ep_expert_product -- every expert's weights times the rows in its window, on the windows that
+ * ep_dispatch has filled.  The row counts are read on the device: no host synchronisation.
+ * handle:  the routing whose windows the row tensors are (concatenated [rows, .] or padded
+ *          [num_experts, C, .], strides as for ep_dispatch); weights of L experts from first_expert on.  Or NULL, and the
+ *          windows come with the call: ROW_COUNT int32 [L] rows of each expert and, for 2-D row tensors,
+ *          ROW_OFFSET int32 [L] its first row; 3-D row tensors [L, C, .] have theirs at [e, 0 .. count).
+ * inputs:  TOKENS x, rows of Kd bf16; EXPERT_WEIGHTS W bf16 [L, N, Kd]; EXPERT_BIAS b f32 or bf16 [L, N]
+ *          (optional); RESIDUAL r, rows like the output (optional).
+ * outputs: TOKENS out, rows of N (gated: N/2) bf16; PREACT, rows of N bf16 (optional): what
+ *          ep_expert_product_backward wants to see again.
+ *     pre = x W_e^T + b_e;  out = act(pre) + r,  or act(pre[:N/2]) * pre[N/2:] + r
+ * with float32 accumulation and one rounding to bf16 (of pre as delivered, and of out).  Rows outside the
+ * windows are left untouched.  Rows of a window beyond the shortest row tensor are skipped and, with a
+ * handle, flagged (status bit 2).  r may be out itself.
+ * N (and N/2), Kd multiples of 8; every row on a 16-byte boundary, rows less than 2^22 elements apart;
+ * a gated expert's weights span less than 2^31 bytes (else EP_ERR_UNSUPPORTED).  One expert is a plain
+ * matrix product with bias, activation and residual.
+ * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED, EP_ERR_HIP.
+ */
+EP_API ep_result_t ep_expert_product(ep_handle_t handle, const ep_product_config_t *cfg, const ep_tensor_t *inputs,
+                                     int32_t num_inputs, const ep_tensor_t *outputs, int32_t num_outputs,
+                                     ep_stream_t stream);
+
+/*
+ * ep_expert_product_backward -- its backward pass on the same windows (handle or ROW_OFFSET / ROW_COUNT).
+ * inputs:  EXPERT_TOKENS g, gradient of out (the residual's gradient is g itself); PREACT pre as delivered
+ *          by the forward call (given exactly when there is an activation or a gate); TOKENS x (needed for
+ *          the weights' gradient); EXPERT_WEIGHTS W (needed for the rows' gradient).
+ * outputs: PREACT grad_pre, rows of N bf16 (given exactly when pre is; may be pre itself): the gradient of
+ *          pre, which the other two products read;
+ *          TOKENS grad_x = grad_pre W_e (optional; may be neither g nor grad_pre);
+ *          EXPERT_WEIGHTS grad_W_e = grad_pre^T x, [L, N, Kd] f32 or bf16 (optional), zeros for an expert
+ *          without rows; EXPERT_BIAS [L, N], of the same type, column sums of grad_pre (optional, only
+ *          with grad_W).
+ * Sums in float32, over the rows in one fixed order.  At least one of W and grad_W is given.
+ * Errors: EP_ERR_INVALID_ARG, EP_ERR_HIP.
+ */
+EP_API ep_result_t ep_expert_product_backward(ep_handle_t handle, const ep_product_config_t *cfg,
+                                              const ep_tensor_t *inputs, int32_t num_inputs,
+                                              const ep_tensor_t *outputs, int32_t num_outputs, ep_stream_t stream);
+
+/* What ep_expert_layer needs for a call (host arithmetic, no GPU). */
+typedef struct {
+    int64_t workspace_bytes;
+    int32_t slots;        /* experts that can be named at most: min(num_experts, num_tokens * top_k)  */
+    int32_t reserved;
+} ep_expert_layer_plan_t;
+EP_API ep_result_t ep_expert_layer_plan(int64_t num_tokens, int32_t top_k, int32_t num_experts, int32_t hidden,
+                                        int32_t inner, ep_expert_layer_plan_t *plan);
+
+/*
+ * ep_expert_layer -- the experts of a whole layer for at most 128 tokens, in two launches and without
+ * windows: for decode steps, which are bound by reading the weights of the experts that are named.
+ * inputs:  TOKENS x bf16 [T, H]; TOPK_IDX int32 [T, K]; TOPK_WEIGHTS w f32 [T, K] (optional, absent = 1);
+ *          EXPERT_WEIGHTS W1 bf16 [L, N, H]; DOWN_WEIGHTS W2 bf16 [L, H, I], I = N (gated: N/2);
+ *          EXPERT_BIAS b1 [L, N] and DOWN_BIAS b2 [L, H], f32 or bf16 (optional);
+ *          RESIDUAL r bf16 [T, H] (optional; may be out itself, as may x).
+ * outputs: TOKENS out bf16 [T, H]; WORKSPACE u8 [workspace_bytes] on a 16-byte boundary: contents
+ *          irrelevant before and after; calls that may overlap in time need one each.
+ *     out[t] = r[t] + sum over k with a local expert of w[t,k] * (W2_e act(W1_e x[t] + b1_e) + b2_e)
+ * e = idx[t,k] - first_expert; ids outside [first_expert, first_expert + L) (-1, other ranks' experts)
+ * contribute nothing.  An expert may be named twice by a token.  w * act(.) is rounded to bf16 between the
+ * two products; sums are float32 in a fixed order.  H and I multiples of 8, at most 2^17.
+ * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED (more than 128 tokens), EP_ERR_HIP.
+ */
+EP_API ep_result_t ep_expert_layer(const ep_product_config_t *cfg, const ep_tensor_t *inputs, int32_t num_inputs,
+                                   const ep_tensor_t *outputs, int32_t num_outputs, ep_stream_t stream);
 
 #ifdef __cplusplus
 }

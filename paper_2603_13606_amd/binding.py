@@ -44,6 +44,20 @@ EP_TAG_TOKENS_PER_EXPERTS = 7
 EP_TAG_RECV_SRC_TOKEN = 8
 EP_TAG_EXPERT_BASE = 9
 EP_TAG_EXPERT_TOKENS = 10
+EP_TAG_LOGITS = 11
+EP_TAG_SELECT_BIAS = 12
+EP_TAG_EXPERT_WEIGHTS = 13
+EP_TAG_EXPERT_BIAS = 14
+EP_TAG_RESIDUAL = 15
+EP_TAG_PREACT = 16
+EP_TAG_ROW_OFFSET = 17
+EP_TAG_ROW_COUNT = 18
+EP_TAG_DOWN_WEIGHTS = 19
+EP_TAG_DOWN_BIAS = 20
+EP_TAG_WORKSPACE = 21
+
+EP_SCORE_SOFTMAX, EP_SCORE_SIGMOID = 0, 1
+EP_ACT_NONE, EP_ACT_SILU, EP_ACT_GELU = 0, 1, 2
 
 STATUS_INVALID_IDS, STATUS_CAPACITY_DROP, STATUS_OUTPUT_OVERFLOW, STATUS_TIMEOUT = 1, 2, 4, 8
 
@@ -51,6 +65,7 @@ EXPORTS = [
     "ep_error_string", "ep_version", "ep_build_id", "ep_layout_plan", "ep_dispatch_plan", "ep_combine_plan", "ep_calibration_copy", "ep_calibration_fill", "ep_calibration_read", "ep_group_create", "ep_group_destroy", "ep_group_query",
     "ep_layout", "ep_layout_prefetch", "ep_layout_static", "ep_layout_dispatch", "ep_handle_query", "ep_handle_get_num_recv_tokens", "ep_handle_destroy",
     "ep_dispatch", "ep_combine", "ep_combine_backward", "ep_combine_backward_full", "ep_complete", "ep_group_reset_signals",
+    "ep_route", "ep_route_backward", "ep_expert_product", "ep_expert_product_backward", "ep_expert_layer_plan", "ep_expert_layer",
 ]
 
 
@@ -86,6 +101,20 @@ class ep_group_info_t(ctypes.Structure):
         ("signals", ctypes.c_void_p * 2), ("combine_staging", ctypes.c_void_p * 2),
         ("msg_stride", ctypes.c_int64), ("msg_lead", ctypes.c_int64),
         ("hint_rows_kept", ctypes.c_int32), ("hint_rows_dropped", ctypes.c_int32)]
+
+
+class ep_route_config_t(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32), ("score", ctypes.c_int32), ("renormalise", ctypes.c_int32),
+                ("num_groups", ctypes.c_int32), ("groups_kept", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class ep_product_config_t(ctypes.Structure):
+    _fields_ = [("size", ctypes.c_uint32), ("activation", ctypes.c_int32), ("gated", ctypes.c_int32),
+                ("first_expert", ctypes.c_int32), ("accumulate", ctypes.c_int32)]
+
+
+class ep_expert_layer_plan_t(ctypes.Structure):
+    _fields_ = [("workspace_bytes", ctypes.c_int64), ("slots", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _INFO_PTRS = ("expert_count", "expert_kept", "expert_offset", "rank_pair_count", "rank_token_count",
@@ -174,6 +203,13 @@ def load() -> ctypes.CDLL:
                                          ctypes.POINTER(ep_dispatch_plan_t)]
         lib.ep_combine_plan.argtypes = [ctypes.POINTER(ep_group_config_t), ctypes.c_int64, ctypes.c_int32,
                                         ctypes.POINTER(ep_combine_plan_t)]
+        tp = ctypes.POINTER(ep_tensor_t)
+        for fn in (lib.ep_route, lib.ep_route_backward):
+            fn.argtypes = [ctypes.POINTER(ep_route_config_t), tp, i32, tp, i32, vp]
+        for fn in (lib.ep_expert_product, lib.ep_expert_product_backward):
+            fn.argtypes = [vp, ctypes.POINTER(ep_product_config_t), tp, i32, tp, i32, vp]
+        lib.ep_expert_layer.argtypes = [ctypes.POINTER(ep_product_config_t), tp, i32, tp, i32, vp]
+        lib.ep_expert_layer_plan.argtypes = [ctypes.c_int64, i32, i32, i32, i32, ctypes.POINTER(ep_expert_layer_plan_t)]
         for name in EXPORTS[3:]:
             getattr(lib, name).restype = ctypes.c_int
         _lib = lib
@@ -545,6 +581,139 @@ class PreparedLayout:
         if code != EP_SUCCESS:
             raise EpError(code, "ep_layout")
         return h
+
+
+# ---------------------------------------------------------------------- the gate, the experts' products, the layer
+
+
+class PreparedOperator:
+    """One call of ep_route, ep_expert_product, ep_expert_layer or a backward pass with its descriptors built once.
+    The tensors must stay alive and keep their shapes; the stream, and the handle where the call was prepared
+    with one, are given per call."""
+
+    def __init__(self, fn_name: str, cfg, ins, outs, takes_handle: bool = False):
+        ins, outs = [p for p in ins if p[0] is not None], [p for p in outs if p[0] is not None]
+        _one_device([t for t, _ in ins + outs])
+        self._fn = getattr(load(), fn_name)
+        self._name = fn_name
+        self._cfg = cfg
+        self._keep = [t for t, _ in ins] + [t for t, _ in outs]
+        self._takes_handle = takes_handle
+        self._args = (ctypes.byref(cfg), _descs(ins), len(ins), _descs(outs), len(outs))
+
+    def __call__(self, handle=None, stream_ptr: int = 0) -> None:
+        code = self._fn(handle, *self._args, stream_ptr) if self._takes_handle else self._fn(*self._args, stream_ptr)
+        if code != EP_SUCCESS:
+            raise EpError(code, self._name)
+
+    def on(self, stream, handle=None) -> None:
+        """The call on a torch stream (None: the current one) or a raw one."""
+        self(handle, _stream_ptr(stream))
+
+
+def _one_device(tensors) -> None:
+    """The library launches on the current device: a tensor of another one is the caller's mistake."""
+    gpu = {t.device for t in tensors if t.is_cuda}
+    if len(gpu) > 1 or (gpu and next(iter(gpu)).index != torch.cuda.current_device()):
+        raise ValueError(f"tensors on {sorted(map(str, gpu))}, current device cuda:{torch.cuda.current_device()}")
+
+
+def _route_config(score, renormalise, num_groups, groups_kept, scale) -> ep_route_config_t:
+    return ep_route_config_t(ctypes.sizeof(ep_route_config_t), int(score), int(renormalise), num_groups, groups_kept, scale)
+
+
+def _product_config(activation, gated, first_expert=0, accumulate=False) -> ep_product_config_t:
+    return ep_product_config_t(ctypes.sizeof(ep_product_config_t), int(activation), int(gated), first_expert, int(accumulate))
+
+
+def prepare_route(logits, topk_idx, topk_weights, bias=None, score=EP_SCORE_SOFTMAX, renormalise=True, num_groups=1, groups_kept=1,
+                  scale=1.0) -> PreparedOperator:
+    return PreparedOperator("ep_route", _route_config(score, renormalise, num_groups, groups_kept, scale),
+                            [(logits, EP_TAG_LOGITS), (bias, EP_TAG_SELECT_BIAS)],
+                            [(topk_idx, EP_TAG_TOPK_IDX), (topk_weights, EP_TAG_TOPK_WEIGHTS)])
+
+
+def prepare_route_backward(logits, topk_idx, grad_w, grad_logits, score=EP_SCORE_SOFTMAX, renormalise=True, scale=1.0) -> PreparedOperator:
+    return PreparedOperator("ep_route_backward", _route_config(score, renormalise, 1, 1, scale),
+                            [(logits, EP_TAG_LOGITS), (topk_idx, EP_TAG_TOPK_IDX), (grad_w, EP_TAG_TOPK_WEIGHTS)],
+                            [(grad_logits, EP_TAG_LOGITS)])
+
+
+def prepare_expert_product(x, weights, out, bias=None, residual=None, pre=None, row_offset=None, row_count=None, activation=EP_ACT_NONE,
+                           gated=False, first_expert=0) -> PreparedOperator:
+    return PreparedOperator("ep_expert_product", _product_config(activation, gated, first_expert),
+                            [(x, EP_TAG_TOKENS), (weights, EP_TAG_EXPERT_WEIGHTS), (bias, EP_TAG_EXPERT_BIAS),
+                             (residual, EP_TAG_RESIDUAL), (row_offset, EP_TAG_ROW_OFFSET), (row_count, EP_TAG_ROW_COUNT)],
+                            [(out, EP_TAG_TOKENS), (pre, EP_TAG_PREACT)], takes_handle=True)
+
+
+def prepare_expert_product_backward(grad_out, weights=None, x=None, pre=None, grad_pre=None, grad_x=None, grad_weights=None,
+                                    grad_bias=None, row_offset=None, row_count=None, activation=EP_ACT_NONE, gated=False,
+                                    first_expert=0, accumulate=False) -> PreparedOperator:
+    return PreparedOperator("ep_expert_product_backward", _product_config(activation, gated, first_expert, accumulate),
+                            [(grad_out, EP_TAG_EXPERT_TOKENS), (weights, EP_TAG_EXPERT_WEIGHTS), (x, EP_TAG_TOKENS),
+                             (pre, EP_TAG_PREACT), (row_offset, EP_TAG_ROW_OFFSET), (row_count, EP_TAG_ROW_COUNT)],
+                            [(grad_pre, EP_TAG_PREACT), (grad_x, EP_TAG_TOKENS), (grad_weights, EP_TAG_EXPERT_WEIGHTS),
+                             (grad_bias, EP_TAG_EXPERT_BIAS)], takes_handle=True)
+
+
+def prepare_expert_layer(x, topk_idx, topk_weights, w_up, w_down, out, workspace, bias_up=None, bias_down=None, residual=None,
+                         activation=EP_ACT_NONE, gated=False, first_expert=0) -> PreparedOperator:
+    return PreparedOperator("ep_expert_layer", _product_config(activation, gated, first_expert),
+                            [(x, EP_TAG_TOKENS), (topk_idx, EP_TAG_TOPK_IDX), (topk_weights, EP_TAG_TOPK_WEIGHTS),
+                             (w_up, EP_TAG_EXPERT_WEIGHTS), (w_down, EP_TAG_DOWN_WEIGHTS), (bias_up, EP_TAG_EXPERT_BIAS),
+                             (bias_down, EP_TAG_DOWN_BIAS), (residual, EP_TAG_RESIDUAL)],
+                            [(out, EP_TAG_TOKENS), (workspace, EP_TAG_WORKSPACE)])
+
+
+def ep_route(logits: torch.Tensor, topk_idx: torch.Tensor, topk_weights: torch.Tensor, bias: Optional[torch.Tensor] = None,
+             score: int = EP_SCORE_SOFTMAX, renormalise: bool = True, num_groups: int = 1, groups_kept: int = 1, scale: float = 1.0,
+             stream=None) -> None:
+    """The gate: the K experts of each token (topk_idx int32 [T, K]) and their weights (f32 [T, K]) from the logits [T, E]."""
+    prepare_route(logits, topk_idx, topk_weights, bias, score, renormalise, num_groups, groups_kept, scale).on(stream)
+
+
+def ep_route_backward(logits: torch.Tensor, topk_idx: torch.Tensor, grad_w: torch.Tensor, grad_logits: torch.Tensor,
+                      score: int = EP_SCORE_SOFTMAX, renormalise: bool = True, scale: float = 1.0, stream=None) -> None:
+    """Gradient of the logits from that of the gate weights, the choice of experts being fixed."""
+    prepare_route_backward(logits, topk_idx, grad_w, grad_logits, score, renormalise, scale).on(stream)
+
+
+def ep_expert_product(x: torch.Tensor, weights: torch.Tensor, out: torch.Tensor, handle=None, bias: Optional[torch.Tensor] = None,
+                      residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                      row_offset: Optional[torch.Tensor] = None, row_count: Optional[torch.Tensor] = None,
+                      activation: int = EP_ACT_NONE, gated: bool = False, first_expert: int = 0, stream=None) -> None:
+    """Each expert's weights times the rows of its window, with bias, activation and residual; the windows are those of
+    `handle`, or come as row_count (and row_offset for 2-D rows)."""
+    prepare_expert_product(x, weights, out, bias, residual, pre, row_offset, row_count, activation, gated, first_expert).on(stream, handle)
+
+
+def ep_expert_product_backward(grad_out: torch.Tensor, weights: Optional[torch.Tensor] = None, handle=None,
+                               x: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None,
+                               grad_pre: Optional[torch.Tensor] = None, grad_x: Optional[torch.Tensor] = None,
+                               grad_weights: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                               row_offset: Optional[torch.Tensor] = None, row_count: Optional[torch.Tensor] = None,
+                               activation: int = EP_ACT_NONE, gated: bool = False, first_expert: int = 0, accumulate: bool = False,
+                               stream=None) -> None:
+    """Gradients of ep_expert_product: of the pre-activation, the rows, the weights and the bias, as far as they are given."""
+    prepare_expert_product_backward(grad_out, weights, x, pre, grad_pre, grad_x, grad_weights, grad_bias, row_offset, row_count,
+                                    activation, gated, first_expert, accumulate).on(stream, handle)
+
+
+def ep_expert_layer_plan(num_tokens: int, top_k: int, num_experts: int, hidden: int, inner: int) -> ep_expert_layer_plan_t:
+    """Workspace that ep_expert_layer needs for such a call (host arithmetic)."""
+    plan = ep_expert_layer_plan_t()
+    _check(load().ep_expert_layer_plan(num_tokens, top_k, num_experts, hidden, inner, ctypes.byref(plan)), "ep_expert_layer_plan")
+    return plan
+
+
+def ep_expert_layer(x: torch.Tensor, topk_idx: torch.Tensor, topk_weights: Optional[torch.Tensor], w_up: torch.Tensor, w_down: torch.Tensor,
+                    out: torch.Tensor, workspace: torch.Tensor, bias_up: Optional[torch.Tensor] = None,
+                    bias_down: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, activation: int = EP_ACT_NONE,
+                    gated: bool = False, first_expert: int = 0, stream=None) -> None:
+    """The experts of a whole layer for at most 128 tokens, without windows."""
+    prepare_expert_layer(x, topk_idx, topk_weights, w_up, w_down, out, workspace, bias_up, bias_down, residual, activation, gated,
+                         first_expert).on(stream)
 
 
 def read_device_i32(ptr: int, n: int) -> torch.Tensor:

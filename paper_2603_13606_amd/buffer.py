@@ -258,6 +258,59 @@ class EPBuffer:
                     t.record_stream(run)
         return grad_y, grad_w, self._leave(compute, run, capturing, grad_y, grad_w)
 
+    # ------------------------------------------------------------------ the gate and the experts
+    # Computation, not communication: these run on the compute stream, whatever stream dispatch and combine take.
+
+    def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, score: str = "softmax", renormalise: bool = True,
+              num_groups: int = 1, groups_kept: int = 1, scale: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
+        """topk_idx, topk_weights = route(logits): the buffer's K experts of each token and their gate weights."""
+        return route(logits, self.K, bias, score, renormalise, num_groups, groups_kept, scale)
+
+    def expert_product(self, x: torch.Tensor, weights: torch.Tensor, handle: EPHandle, bias: Optional[torch.Tensor] = None,
+                       residual: Optional[torch.Tensor] = None, activation: str = "none", gated: bool = False, keep_pre: bool = False,
+                       first_expert: int = 0):
+        """out, pre = expert_product(x, weights, handle): every expert's weights [L, N, Kd] times the rows of x in its window
+        (of experts first_expert on), with bias, activation and residual.  pre, the rows before the activation, is what the
+        backward pass wants (None unless keep_pre).  Rows outside the windows are not written."""
+        N = weights.shape[1]
+        out = torch.empty((*x.shape[:-1], N // 2 if gated else N), dtype=torch.bfloat16, device=x.device)
+        pre = torch.empty((*x.shape[:-1], N), dtype=torch.bfloat16, device=x.device) if keep_pre else None
+        with self._lock:
+            self._behind_calls()
+            ep.ep_expert_product(x, weights, out, handle=handle.raw, bias=bias, residual=residual, pre=pre, activation=_ACTS[activation],
+                                 gated=gated, first_expert=first_expert)
+        return out, pre
+
+    def expert_product_backward(self, grad_out: torch.Tensor, handle: EPHandle, weights: Optional[torch.Tensor] = None,
+                                x: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, activation: str = "none",
+                                gated: bool = False, grad_weights: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                                accumulate: bool = False, first_expert: int = 0):
+        """grad_x, grad_pre = expert_product_backward(grad_out, handle, weights, x, pre): the gradient of the rows (given the
+        weights; zeros outside the windows) and of the pre-activation; gradients of weights and bias go to the tensors given
+        for them (bf16 or float32), or are added to what they hold."""
+        shape = (weights if weights is not None else grad_weights).shape
+        grad_pre = torch.empty_like(pre) if pre is not None else None
+        grad_x = torch.zeros((*grad_out.shape[:-1], shape[2]), dtype=torch.bfloat16, device=grad_out.device) if weights is not None else None
+        with self._lock:
+            self._behind_calls()
+            ep.ep_expert_product_backward(grad_out, weights, handle=handle.raw, x=x, pre=pre, grad_pre=grad_pre, grad_x=grad_x,
+                                          grad_weights=grad_weights, grad_bias=grad_bias, activation=_ACTS[activation], gated=gated,
+                                          first_expert=first_expert, accumulate=accumulate)
+        return grad_x, grad_pre
+
+    def expert_layer(self, x: torch.Tensor, topk_idx: torch.Tensor, topk_weights: Optional[torch.Tensor], w_up: torch.Tensor,
+                     w_down: torch.Tensor, bias_up: Optional[torch.Tensor] = None, bias_down: Optional[torch.Tensor] = None,
+                     residual: Optional[torch.Tensor] = None, activation: str = "silu", gated: bool = True, first_expert: int = 0):
+        """out = expert_layer(x, topk_idx, topk_weights, w_up, w_down): the experts of a whole layer for at most 128 tokens,
+        without dispatch and combine."""
+        return expert_layer(x, topk_idx, topk_weights, w_up, w_down, bias_up, bias_down, residual, activation, gated, first_expert)
+
+    def _behind_calls(self) -> None:
+        """The compute stream waits for the calls made so far, if it has not yet (the windows' row counts are read there)."""
+        compute = torch.cuda.current_stream()
+        if self._order_event is not None and compute.cuda_stream not in self._order_streams and not torch.cuda.is_current_stream_capturing():
+            compute.wait_event(self._order_event)
+
     def get_tokens_per_expert_list(self) -> List[int]:
         """Rows placed per expert by the last dispatch, read from the pinned counter."""
         if self._last_event is not None:
@@ -308,7 +361,84 @@ def _device_pointer_of_pinned(t: torch.Tensor) -> int:
     return int(dev.value)
 
 
+# ---------------------------------------------------------------------- the gate and the layer without a buffer
+
+_ACTS = {"none": ep.EP_ACT_NONE, "silu": ep.EP_ACT_SILU, "gelu": ep.EP_ACT_GELU}
+_SCORES = {"softmax": ep.EP_SCORE_SOFTMAX, "sigmoid": ep.EP_SCORE_SIGMOID}
+
+
+def route(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None, score: str = "softmax", renormalise: bool = True,
+          num_groups: int = 1, groups_kept: int = 1, scale: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """topk_idx int32 [T, K], topk_weights float32 [T, K] from the gate's logits [T, E] (float32 or bf16)."""
+    idx = torch.empty((logits.shape[0], top_k), dtype=torch.int32, device=logits.device)
+    w = torch.empty((logits.shape[0], top_k), dtype=torch.float32, device=logits.device)
+    ep.ep_route(logits, idx, w, bias, _SCORES[score], renormalise, num_groups, groups_kept, scale)
+    return idx, w
+
+
+def expert_layer(x: torch.Tensor, topk_idx: torch.Tensor, topk_weights: Optional[torch.Tensor], w_up: torch.Tensor, w_down: torch.Tensor,
+                 bias_up: Optional[torch.Tensor] = None, bias_down: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None,
+                 activation: str = "silu", gated: bool = True, first_expert: int = 0) -> torch.Tensor:
+    """The experts of a whole layer for at most 128 tokens; the workspace comes from torch's allocator, per call."""
+    out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    need = ep.ep_expert_layer_plan(x.shape[0], topk_idx.shape[1], w_up.shape[0], x.shape[1], w_down.shape[2]).workspace_bytes
+    workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+    ep.ep_expert_layer(x, topk_idx, topk_weights, w_up, w_down, out, workspace, bias_up, bias_down, residual, _ACTS[activation], gated,
+                       first_expert)
+    return out
+
+
 # ---------------------------------------------------------------------- autograd wrappers
+
+
+class EPRouteFn(torch.autograd.Function):
+    """Forward: the gate.  Backward: gradient of the logits with the choice of experts fixed; the selection bias has none."""
+
+    @staticmethod
+    def forward(ctx, logits, top_k, bias=None, score="softmax", renormalise=True, num_groups=1, groups_kept=1, scale=1.0):
+        idx, w = route(logits, top_k, bias, score, renormalise, num_groups, groups_kept, scale)
+        ctx.save_for_backward(logits, idx)
+        ctx.rule = dict(score=_SCORES[score], renormalise=renormalise, scale=scale)
+        ctx.mark_non_differentiable(idx)
+        return idx, w
+
+    @staticmethod
+    def backward(ctx, _, grad_w):
+        logits, idx = ctx.saved_tensors
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        ep.ep_route_backward(logits, idx, grad_w.contiguous(), grad, **ctx.rule)
+        return (grad,) + (None,) * 7
+
+
+class EPExpertProductFn(torch.autograd.Function):
+    """Forward: the experts' product on a handle's windows.  Backward: the gradients of rows, weights, bias and residual
+    with the same handle."""
+
+    @staticmethod
+    def forward(ctx, x, weights, bias, residual, buf: EPBuffer, handle: EPHandle, activation="none", gated=False):
+        keep = activation != "none" or gated
+        out, pre = buf.expert_product(x, weights, handle, bias, residual, activation, gated, keep_pre=keep)
+        ctx.save_for_backward(x, weights, pre)
+        ctx.buf, ctx.handle, ctx.activation, ctx.gated = buf, handle, activation, gated
+        ctx.bias_type = bias.dtype if bias is not None else None
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        x, weights, pre = ctx.saved_tensors
+        grad_out = grad_out.contiguous()
+        need_x, need_w, need_b, need_r = ctx.needs_input_grad[:4]
+        gx = gw = gb = None
+        if need_x or need_w or need_b:
+            # weights and bias: one kernel makes both, in one type; float32 where the bias wants it
+            wide = ctx.bias_type == torch.float32
+            if need_w or need_b:
+                gw = torch.empty(weights.shape, dtype=torch.float32 if wide else torch.bfloat16, device=weights.device)
+            if need_b:
+                gb = torch.empty(weights.shape[:2], dtype=gw.dtype, device=weights.device)
+            gx, _ = ctx.buf.expert_product_backward(grad_out, ctx.handle, weights if need_x else None, x, pre, ctx.activation, ctx.gated,
+                                                    grad_weights=gw, grad_bias=gb)
+        return (gx, gw.to(weights.dtype) if need_w else None, gb if need_b else None, grad_out if need_r else None, None, None, None, None)
 
 
 class EPDispatchFn(torch.autograd.Function):

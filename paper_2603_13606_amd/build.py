@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libep_mi355x.so")
-SOURCES = ["ep_api.hip", "ep_layout.hip", "ep_dispatch.hip", "ep_dedup.hip", "ep_combine.hip", "ep_staged.hip"]
+SOURCES = ["ep_api.hip", "ep_layout.hip", "ep_dispatch.hip", "ep_dedup.hip", "ep_combine.hip", "ep_staged.hip",
+           "ep_route.hip", "ep_product.hip", "ep_layer.hip", "ep_experts_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off on purpose: some of their forms have
@@ -21,7 +22,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 
-HEADERS = [os.path.join(CSRC, "ep_internal.h"), os.path.join(CSRC, "ep_fp8.h"), os.path.join(ROOT, "include", "ep.h")]
+HEADERS = [os.path.join(CSRC, "ep_internal.h"), os.path.join(CSRC, "ep_fp8.h"), os.path.join(CSRC, "ep_check.h"),
+           os.path.join(CSRC, "ep_experts.h"), os.path.join(ROOT, "include", "ep.h")]
 _ID_MARK = b"EP_BUILD_ID="
 
 
@@ -69,7 +71,7 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = False) -> str:
     """Compile every source and link the shared library; always recompiles."""
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, SOURCES))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

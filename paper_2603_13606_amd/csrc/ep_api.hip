@@ -7,6 +7,7 @@
 #include <new>
 #include <vector>
 
+#include "ep_check.h"
 #include "ep_internal.h"
 
 using namespace ep;
@@ -218,32 +219,10 @@ ep_result_t new_slab(ep_group_s* g, Slab* s, hipStream_t stream) {
     return EP_SUCCESS;
 }
 
-const ep_tensor_t* find_tag(const ep_tensor_t* ts, int n, int tag, int tag2 = -1, int tag3 = -1) {
-    for (int i = 0; i < n; ++i)
-        if (ts[i].tag == tag || ts[i].tag == tag2 || ts[i].tag == tag3) return &ts[i];
-    return nullptr;
-}
-
 bool has_scales(const ep_tensor_t* ts, int n) {
     for (int i = 0; i < n; ++i)
         if (ts[i].tag == EP_TAG_SCALES) return true;
     return false;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
-// 2-D [rows, cols] tensor of `dtype`, innermost stride 1.
-bool check_2d(const ep_tensor_t* t, int dtype, int64_t rows, int64_t cols, bool rows_exact) {
-    if (!t || t->ndim != 2 || t->dtype != dtype) return false;
-    if (t->shape[1] != cols || t->stride[1] != 1 || t->stride[0] < cols) return false;
-    if (rows_exact ? t->shape[0] != rows : t->shape[0] < rows) return false;
-    if (t->shape[0] > 0 && !t->data) return false;
-    return true;
-}
-
-bool check_1d(const ep_tensor_t* t, int dtype, int64_t n) {
-    if (!t || t->ndim != 1 || t->dtype != dtype || t->shape[0] < n || t->stride[0] != 1) return false;
-    return t->data != nullptr || t->shape[0] == 0;
 }
 
 // Token windows: HT [rows_cap, H]; LL [E, C, H].  Fills a WindowDesc.  Rows must start on
@@ -346,6 +325,22 @@ ep_result_t static_scratch(int32_t** out) {
 
 }  // namespace
 
+namespace ep {
+
+void handle_rows(ep_handle_t h, HandleRows* out) {
+    const ep_group_s* g = h->group;
+    out->experts = g->cfg.num_experts;
+    out->padded = g->cfg.mode == EP_MODE_LL;
+    out->slots = g->C;
+    out->offset = h->slab.expert_offset;
+    out->kept = h->slab.expert_kept;
+    out->status = h->slab.totals + TOT_STATUS;
+}
+
+void handle_used(ep_handle_t h, hipStream_t stream) { h->last_stream = stream; }
+
+}  // namespace ep
+
 extern "C" {
 
 const char* ep_error_string(ep_result_t code) {
@@ -363,7 +358,7 @@ const char* ep_error_string(ep_result_t code) {
     return "unknown error code";
 }
 
-int32_t ep_version(void) { return 401; }  // 0.4.1: ep_combine_backward_full added (0.4.0: calibration fill / read and ep_combine_plan added; 0.3.0: ep_group_config_t and ep_group_info_t grew)
+int32_t ep_version(void) { return 500; }  // 0.5.0: the gate, the experts' products and the layer of few tokens added (0.4.1: ep_combine_backward_full added; 0.4.0: calibration fill / read and ep_combine_plan added; 0.3.0: ep_group_config_t and ep_group_info_t grew)
 
 #ifndef EP_BUILD_ID_STRING
 #define EP_BUILD_ID_STRING "unknown"

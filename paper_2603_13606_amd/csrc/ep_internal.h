@@ -218,6 +218,16 @@ struct DedupRankArgs {
     int padded, C;
 };
 
+// The row windows of a handle, for operators that work on them.
+struct HandleRows {
+    int experts, padded, slots;   // padded: [experts, slots] rows
+    const int32_t *offset, *kept; // [experts] first row and number of rows
+    int32_t* status;
+};
+void handle_rows(ep_handle_t h, HandleRows* out);
+// The handle remembers `stream` as that of its last call.
+void handle_used(ep_handle_t h, hipStream_t stream);
+
 hipError_t launch_layout(const LayoutArgs& a, hipStream_t s);
 // Layout and direct dispatch of a small input in one launch (see ep_layout.hip); `fusable` says
 // whether the pair qualifies.

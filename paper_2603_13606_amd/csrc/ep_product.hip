@@ -1,0 +1,535 @@
+// The experts' products: rows in expert windows times that expert's weights, forward and backward.
+//
+//   forward    out[r, :]  = act(x[r, :] W_e^T + b_e) (+ res[r, :])            W_e [N, Kd]
+//   gradients  grad_x     = grad_pre W_e
+//              grad_W_e   = grad_pre_e^T x_e,  grad_b_e = column sums of grad_pre_e
+//
+// All three are one tiled kernel over MFMA 16x16x32 with float32 accumulators.  The matrix instruction
+// leaves each lane four consecutive rows of one column of its result, so the operand that runs along the
+// contiguous axis of the output (P) is given as its left one and the other (Q) as its right one: a lane
+// then owns four neighbouring values of an output row.  An operand whose contraction index is contiguous
+// in memory is read from LDS 16 bytes per lane; one whose contraction index is the row (the weights of
+// grad_x, both operands of grad_W) goes through the transposing LDS read.
+#include <algorithm>
+#include <atomic>
+
+#include "ep_experts.h"
+#include "ep_internal.h"
+
+namespace ep {
+
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+constexpr int kBK = 64;                       // contraction indices per LDS tile
+constexpr uint32_t kNowhere = 0x80000000u;    // offset of a lane that has nothing to load: beyond the buffer's end, gives zeros
+
+enum { FORWARD = 0, GRAD_ROWS = 1, GRAD_WEIGHTS = 2 };
+
+// What the three kernels have in common.
+struct Product {
+    Windows win;
+    const uint16_t *p, *q;
+    int64_t p_expert, p_row, q_expert, q_row;
+    uint16_t* out;
+    int64_t out_expert, out_row;
+    int I, J, Kc;        // extents along P, along Q (grad_W) and of the contraction (not grad_W)
+    // forward
+    int act, gated;
+    const void* bias;
+    int64_t bias_stride;
+    int bias_f32;
+    uint16_t *pre, *res;
+    int64_t pre_expert, pre_row, res_expert, res_row;
+    int32_t* status;
+    // grad_W
+    int out_f32, accumulate;
+    void* grad_b;
+    int64_t gb_stride;
+};
+
+// Rows of expert e, cut to what the tensors hold, and the first of them.
+__device__ __forceinline__ int window_rows(const Windows& w, int e, int64_t* first) {
+    int64_t at = w.offset ? w.offset[e] : 0;
+    int64_t n = w.count[e];
+    if (n < 0 || at < 0 || at >= w.cap) n = 0;
+    else if (n > w.cap - at) n = w.cap - at;
+    *first = n > 0 ? at : 0;
+    return (int)n;
+}
+
+// starts[e] = blocks of `rows` rows before expert e, starts[L] = all of them; one wavefront.  Returns
+// whether a window reaches beyond its tensor.
+__device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, int* starts, int lane) {
+    const int per = (w.L + 63) / 64;
+    const int e0 = lane * per, e1 = min(w.L, e0 + per);
+    int sum = 0;
+    bool cut = false;
+    for (int e = e0; e < e1; ++e) {
+        int64_t at;
+        const int n = window_rows(w, e, &at);
+        cut |= n < w.count[e];
+        sum += (n + rows - 1) / rows;
+    }
+    int before = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int v = __shfl_up(before, d);
+        if (lane >= d) before += v;
+    }
+    int at = before - sum;
+    for (int e = e0; e < e1; ++e) {
+        int64_t first;
+        starts[e] = at;
+        at += (window_rows(w, e, &first) + rows - 1) / rows;
+    }
+    if (lane == 63) starts[w.L] = before;
+    return __any(cut);
+}
+
+// The expert whose blocks hold block b: starts[e] <= b < starts[e + 1].
+__device__ __forceinline__ int find_expert(const int* starts, int L, int b) {
+    int lo = 0, hi = L;  // the answer is in [lo, hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (starts[mid] <= b) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// ---- operand tiles -------------------------------------------------------------------------
+//
+// A tile is B indices x 64 contraction indices of bf16.  Contraction contiguous (KM): B rows of 128 bytes,
+// 16-byte unit u of row r stored at u ^ (r & 7), so that the 16 rows of a fragment read touch all banks.
+// Contraction along the rows: 64 rows of 2B bytes, the 32-byte block b of row k stored at b ^ f(k),
+// f(k) = k[1:0] | k[3] << 2: the eight rows that a transposing read takes at a time lie in different banks.
+
+__device__ __forceinline__ int spread(int k) { return (k & 3) | ((k >> 1) & 4); }
+
+template <int B, bool KM, int NT>
+struct Operand {
+    static constexpr int kLoads = B * 8 / NT;
+    static constexpr int kBytes = B * kBK * 2;
+    uint32_t off[kLoads];
+    const uint16_t* base;     // of the current contraction step
+    int64_t step;             // elements per contraction step
+
+    // rows_of(r): the source row of tile row r relative to base, or -1 (contraction contiguous)
+    template <class F>
+    __device__ __forceinline__ void start_rows(const uint16_t* at, int64_t stride, F rows_of) {
+        static_assert(KM, "");
+        base = at;
+        step = kBK;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int u = threadIdx.x + j * NT, r = u >> 3, c = (u & 7) ^ (r & 7);
+            const int src = rows_of(r);
+            off[j] = src < 0 ? kNowhere : (uint32_t)(src * stride * 2) + c * 16;
+        }
+    }
+    __device__ __forceinline__ void start_cols(const uint16_t* at, int64_t stride, int cols) {
+        static_assert(!KM, "");
+        base = at;
+        step = kBK * stride;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int u = threadIdx.x + j * NT, k = u / (B / 8), c = (u % (B / 8)) ^ (spread(k) << 1);
+            off[j] = c * 8 < cols ? (uint32_t)(k * stride * 2) + c * 16 : kNowhere;
+        }
+    }
+    // Loads the tile of the next contraction step; `left` = contraction indices that remain.
+    __device__ __forceinline__ void load(char* lds, int left, int wave) {
+        auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00027000);
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int u = threadIdx.x + j * NT;
+            const int k = KM ? (((u & 7) ^ ((u >> 3) & 7)) * 8) : u / (B / 8);
+            const uint32_t o = k < left ? off[j] : kNowhere;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + (j * NT + wave * 64) * 16), 16, o, 0, 0, 0);
+        }
+        base += step;
+    }
+};
+
+// Fragment of 16 indices from `at` on and 32 contraction indices (half `ks` of the tile).
+template <int B, bool KM>
+__device__ __forceinline__ bf16x8 fragment(const char* lds, int at, int ks, int lane) {
+    if constexpr (KM) {
+        const int r = at + (lane & 15), c = ks * 4 + (lane >> 4);
+        return *(const bf16x8*)(lds + r * 128 + ((c ^ (r & 7)) << 4));
+    } else {
+        const int k = ks * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
+        const int col = at + (lane & 3) * 4;
+        s16x4 v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int kk = k + 4 * h;
+            const char* p = lds + kk * (B * 2) + (((col >> 3) ^ (spread(kk) << 1)) << 4) + (col & 7) * 2;
+            v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
+        }
+        const s16x8 both = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(bf16x8, both);
+    }
+}
+
+__device__ __forceinline__ f32x4 load4(const void* p, int64_t i, int is_f32) {
+    f32x4 v;
+    if (is_f32) {
+        v = *(const f32x4*)((const float*)p + i);
+    } else {
+        const u32x2 u = *(const u32x2*)((const uint16_t*)p + i);
+        v = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16),
+                  __uint_as_float(u[1] & 0xffff0000u)};
+    }
+    return v;
+}
+
+__device__ __forceinline__ void store4(uint16_t* p, const f32x4& v) {
+    *(u32x2*)p = u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+}
+
+template <int KIND, int BI, int BJ, int NWI, int NWJ>
+__global__ __launch_bounds__(64 * NWI * NWJ) void product_kernel(const Product a) {
+    constexpr int NT = 64 * NWI * NWJ;
+    constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
+    constexpr int WI = BI / NWI, WJ = BJ / NWJ, IT = WI / 16, JT = WJ / 16;
+    using P = Operand<BI, kPK, NT>;
+    using Q = Operand<BJ, kQK, NT>;
+    constexpr int kStage = P::kBytes + Q::kBytes;
+    constexpr int kLoads = P::kLoads + Q::kLoads;
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    int* starts = (int*)(lds + 2 * kStage);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wi = wave % NWI, wj = wave / NWI;
+
+    // Tiles: blocks of BJ rows of the experts that have rows (grad_W: of BJ weight rows, for every expert),
+    // times blocks along I.  A gated tile holds BI/2 outputs: their gate and their up columns.
+    const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
+    const int ni = (a.I + bi - 1) / bi;
+    int nj;
+    if (KIND == GRAD_WEIGHTS) {
+        nj = a.win.L * ((a.J + BJ - 1) / BJ);
+    } else {
+        if (wave == 0) {
+            const bool cut = scan_blocks(a.win, BJ, starts, lane);
+            if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && lane == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
+        }
+        __syncthreads();
+        nj = __builtin_amdgcn_readfirstlane(starts[a.win.L]);
+    }
+    const int64_t tiles = (int64_t)nj * ni;
+
+    // Workgroups of one XCD (blockIdx mod 8) take neighbouring tiles, eight row blocks by a few column
+    // blocks, so that its L2 serves both operands.
+    const int per = gridDim.x >> 3;
+    for (int64_t t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3); t < tiles; t += gridDim.x) {
+        const int64_t band = t / (8 * (int64_t)ni);
+        const int height = (int)min((int64_t)8, nj - band * 8);
+        const int in = (int)(t - band * 8 * ni);
+        const int jb = __builtin_amdgcn_readfirstlane((int)(band * 8) + in % height);
+        const int ib = __builtin_amdgcn_readfirstlane(in / height);
+        int e, j0;
+        if (KIND == GRAD_WEIGHTS) {
+            const int per_expert = (a.J + BJ - 1) / BJ;
+            e = jb / per_expert;
+            j0 = (jb - e * per_expert) * BJ;
+        } else {
+            e = __builtin_amdgcn_readfirstlane(find_expert(starts, a.win.L, jb));
+            j0 = (jb - __builtin_amdgcn_readfirstlane(starts[e])) * BJ;
+        }
+        int64_t first;
+        const int rows = window_rows(a.win, e, &first);
+        const int i0 = ib * bi;
+        const int Kc = KIND == GRAD_WEIGHTS ? rows : a.Kc;
+        const int J = KIND == GRAD_WEIGHTS ? a.J : rows;
+
+        P p;
+        Q q;
+        if constexpr (KIND == FORWARD) {
+            const int I = a.I, gated = a.gated;
+            p.start_rows(a.p + e * a.p_expert + i0 * a.p_row, a.p_row, [=](int r) {
+                if (!gated) return i0 + r < I ? r : -1;
+                const int at = (r / WI) * (WI / 2) + r % (WI / 2);           // output column of the tile
+                return i0 + at < I ? at + ((r % WI) / (WI / 2)) * I : -1;    // second half of a wave's rows: up
+            });
+        } else if constexpr (KIND == GRAD_ROWS) {
+            p.start_cols(a.p + e * a.p_expert + i0, a.p_row, a.I - i0);
+        } else {
+            p.start_cols(a.p + e * a.p_expert + first * a.p_row + i0, a.p_row, a.I - i0);
+        }
+        const uint16_t* qb = a.q + e * a.q_expert + first * a.q_row;
+        if constexpr (kQK) q.start_rows(qb + j0 * a.q_row, a.q_row, [=](int r) { return j0 + r < rows ? r : -1; });
+        else q.start_cols(qb + j0, a.q_row, a.J - j0);
+
+        f32x4 acc[IT][JT];
+        f32x4 sums[JT];
+#pragma unroll
+        for (int jt = 0; jt < JT; ++jt) {
+            sums[jt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int it = 0; it < IT; ++it) acc[it][jt] = f32x4{0, 0, 0, 0};
+        }
+        const bool with_sums = KIND == GRAD_WEIGHTS && a.grad_b && ib == 0 && wi == 0;
+
+        const int steps = (Kc + kBK - 1) / kBK;
+        if (steps) {
+            p.load(lds, Kc, wave);
+            q.load(lds + P::kBytes, Kc, wave);
+        }
+        for (int k = 0; k < steps; ++k) {
+            char* cur = lds + (k & 1) * kStage;
+            if (k + 1 < steps) {
+                char* nxt = lds + ((k + 1) & 1) * kStage;
+                p.load(nxt, Kc - (k + 1) * kBK, wave);
+                q.load(nxt + P::kBytes, Kc - (k + 1) * kBK, wave);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+            __builtin_amdgcn_s_barrier();
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                bf16x8 pf[IT], qf[JT];
+#pragma unroll
+                for (int it = 0; it < IT; ++it) pf[it] = fragment<BI, kPK>(cur, wi * WI + it * 16, ks, lane);
+#pragma unroll
+                for (int jt = 0; jt < JT; ++jt) qf[jt] = fragment<BJ, kQK>(cur + P::kBytes, wj * WJ + jt * 16, ks, lane);
+#pragma unroll
+                for (int it = 0; it < IT; ++it)
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt)
+                        acc[it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[it], qf[jt], acc[it][jt], 0, 0, 0);
+                if (with_sums) {  // sums over the rows as a product with ones
+                    const s16x8 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt)
+                        sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[jt], sums[jt], 0, 0, 0);
+                }
+            }
+            // every wave has read the tile before anybody loads into its place
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+        }
+
+        // Results: lane l holds, for index j = l % 16 of a fragment of Q, the indices i = 4 (l / 16) .. + 3 of one of P.
+        const int jl = lane & 15, il = (lane >> 4) * 4;
+        if constexpr (KIND == FORWARD) {
+            const int64_t ob = e * a.out_expert + first * a.out_row, pb = e * a.pre_expert + first * a.pre_row,
+                          rb = e * a.res_expert + first * a.res_row;
+            const char* bias = a.bias ? (const char*)a.bias + e * a.bias_stride * (a.bias_f32 ? 4 : 2) : nullptr;
+            const int nit = a.gated ? IT / 2 : IT;
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                if (it >= nit) continue;
+                const int i = i0 + wi * (a.gated ? WI / 2 : WI) + it * 16 + il;
+                if (i >= a.I) continue;
+                f32x4 b = {0, 0, 0, 0}, bu = {0, 0, 0, 0};
+                if (bias) {
+                    b = load4(bias, i, a.bias_f32);
+                    if (a.gated) bu = load4(bias, i + a.I, a.bias_f32);
+                }
+#pragma unroll
+                for (int jt = 0; jt < JT; ++jt) {
+                    const int j = j0 + wj * WJ + jt * 16 + jl;
+                    if (j >= J) continue;
+                    f32x4 v, up;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = acc[it][jt][r] + b[r];
+                    if (a.gated) {
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) up[r] = acc[(it + IT / 2) % IT][jt][r] + bu[r];
+                    }
+                    if (a.pre) {
+                        uint16_t* at = a.pre + pb + j * a.pre_row + i;
+                        store4(at, v);
+                        if (a.gated) store4(at + a.I, up);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        v[r] = activate(a.act, v[r]);
+                        if (a.gated) v[r] *= up[r];
+                    }
+                    if (a.res) {
+                        const f32x4 res = load4(a.res + rb + j * a.res_row, i, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] += res[r];
+                    }
+                    store4(a.out + ob + j * a.out_row + i, v);
+                }
+            }
+        } else if constexpr (KIND == GRAD_ROWS) {
+            const int64_t ob = e * a.out_expert + first * a.out_row;
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = i0 + wi * WI + it * 16 + il;
+                if (i >= a.I) continue;
+#pragma unroll
+                for (int jt = 0; jt < JT; ++jt) {
+                    const int j = j0 + wj * WJ + jt * 16 + jl;
+                    if (j < J) store4(a.out + ob + j * a.out_row + i, acc[it][jt]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int jt = 0; jt < JT; ++jt) {
+                const int j = j0 + wj * WJ + jt * 16 + jl;
+                if (j >= J) continue;
+                if (with_sums && il == 0) {
+                    const int64_t at = e * a.gb_stride + j;
+                    if (a.out_f32) {
+                        float* g = (float*)a.grad_b + at;
+                        *g = a.accumulate ? *g + sums[jt][0] : sums[jt][0];
+                    } else {
+                        uint16_t* g = (uint16_t*)a.grad_b + at;
+                        *g = (uint16_t)pack2_bf16(a.accumulate ? bf16_f32(*g) + sums[jt][0] : sums[jt][0], 0.0f);
+                    }
+                }
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+                    const int i = i0 + wi * WI + it * 16 + il;
+                    if (i >= a.I) continue;
+                    const int64_t at = e * a.out_expert + j * a.out_row + i;
+                    f32x4 v = acc[it][jt];
+                    if (a.accumulate) {
+                        const f32x4 old = load4(a.out, at, a.out_f32);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) v[r] += old[r];
+                    }
+                    if (a.out_f32) *(f32x4*)((float*)a.out + at) = v;
+                    else store4(a.out + at, v);
+                }
+            }
+        }
+    }
+}
+
+// grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows.
+constexpr int kActRows = 16;
+
+__device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        f[2 * c] = __uint_as_float(w[c] << 16);
+        f[2 * c + 1] = __uint_as_float(w[c] & 0xffff0000u);
+    }
+}
+
+__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+    return make_uint4(pack2_bf16(f[0], f[1]), pack2_bf16(f[2], f[3]), pack2_bf16(f[4], f[5]), pack2_bf16(f[6], f[7]));
+}
+
+__global__ __launch_bounds__(256) void act_backward_kernel(const ActBackwardArgs a) {
+    __shared__ int starts[kMaxExperts + 1];
+    if (threadIdx.x < 64) scan_blocks(a.win, kActRows, starts, threadIdx.x);
+    __syncthreads();
+    const int units = a.No / 8;
+    for (int b = blockIdx.x; b < starts[a.win.L]; b += gridDim.x) {
+        const int e = find_expert(starts, a.win.L, b);
+        int64_t first;
+        const int rows = window_rows(a.win, e, &first), r0 = (b - starts[e]) * kActRows, n = min(kActRows, rows - r0);
+        for (int i = threadIdx.x; i < n * units; i += 256) {
+            const int r = r0 + i / units, c = (i % units) * 8;
+            const uint16_t* pre = a.pre.base + e * a.pre.expert_stride + (first + r) * a.pre.row_stride + c;
+            uint16_t* gp = a.grad_pre.base + e * a.grad_pre.expert_stride + (first + r) * a.grad_pre.row_stride + c;
+            float g[8], v[8], u[8], o[8];
+            unpack8(*(const uint4*)(a.grad_out.base + e * a.grad_out.expert_stride + (first + r) * a.grad_out.row_stride + c), g);
+            unpack8(*(const uint4*)pre, v);
+            if (a.gated) unpack8(*(const uint4*)(pre + a.No), u);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float value;
+                const float d = activate_grad(a.act, v[k], &value);
+                o[k] = g[k] * d * (a.gated ? u[k] : 1.0f);
+                u[k] = g[k] * value;
+            }
+            *(uint4*)gp = pack8(o);
+            if (a.gated) *(uint4*)(gp + a.No) = pack8(u);
+        }
+    }
+}
+
+// Blocks of `rows` rows that there can be at most: every expert's last one may be short.
+int64_t most_blocks(const Windows& w, int rows) {
+    if (!w.offset) return (int64_t)w.L * ((w.cap + rows - 1) / rows);
+    return w.cap / rows + w.L;
+}
+
+template <int KIND>
+hipError_t launch(const Product& a, int64_t most_rows_blocks_128, hipStream_t s) {
+    constexpr int BI = 128, BJ = 128, NWI = 2, NWJ = 2;
+    constexpr int lds = 2 * (BI + BJ) * kBK * 2 + (kMaxExperts + 1) * 4;
+    auto kernel = product_kernel<KIND, BI, BJ, NWI, NWJ>;
+    const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
+    const int64_t most = most_rows_blocks_128 * ((a.I + bi - 1) / bi);
+    if (most <= 0) return hipSuccess;
+    const int64_t cus = std::max(8, compute_units() / 8 * 8);
+    const int64_t grid = std::min(2 * cus, (most + 7) / 8 * 8);  // two workgroups fit a compute unit's LDS
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(64 * NWI * NWJ), lds, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int compute_units() {
+    static std::atomic<int> known[64];
+    int dev = -1, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0) return 256;
+    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) return 256;
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
+    Product p = {};
+    p.win = a.win;
+    p.p = a.w; p.p_expert = a.w_expert; p.p_row = a.w_row;
+    p.q = a.x.base; p.q_expert = a.x.expert_stride; p.q_row = a.x.row_stride;
+    p.out = a.out.base; p.out_expert = a.out.expert_stride; p.out_row = a.out.row_stride;
+    p.I = a.No; p.Kc = a.Kd;
+    p.act = a.act; p.gated = a.gated;
+    p.bias = a.bias; p.bias_stride = a.bias_stride; p.bias_f32 = a.bias_f32;
+    p.pre = a.pre.base; p.pre_expert = a.pre.expert_stride; p.pre_row = a.pre.row_stride;
+    p.res = a.res.base; p.res_expert = a.res.expert_stride; p.res_row = a.res.row_stride;
+    p.status = a.status;
+    return launch<FORWARD>(p, most_blocks(a.win, 128), s);
+}
+
+hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
+    Product p = {};
+    p.win = a.win;
+    p.p = a.w; p.p_expert = a.w_expert; p.p_row = a.w_row;
+    p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
+    p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
+    p.I = a.Kd; p.Kc = a.N;
+    return launch<GRAD_ROWS>(p, most_blocks(a.win, 128), s);
+}
+
+hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
+    Product p = {};
+    p.win = a.win;
+    p.p = a.x.base; p.p_expert = a.x.expert_stride; p.p_row = a.x.row_stride;
+    p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
+    p.out = (uint16_t*)a.grad_w; p.out_expert = a.gw_expert; p.out_row = a.gw_row;
+    p.out_f32 = a.gw_f32; p.accumulate = a.accumulate;
+    p.grad_b = a.grad_b; p.gb_stride = a.gb_stride;
+    p.I = a.Kd; p.J = a.N;
+    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + 127) / 128), s);
+}
+
+hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s) {
+    const int64_t most = most_blocks(a.win, kActRows);
+    if (most <= 0) return hipSuccess;
+    hipLaunchKernelGGL(act_backward_kernel, dim3((uint32_t)std::min<int64_t>(most, 8 * (int64_t)compute_units())), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace ep
