@@ -106,74 +106,91 @@ __device__ __forceinline__ int find_expert(const int* starts, int L, int b) {
 
 // ---- operand tiles -------------------------------------------------------------------------
 //
-// A tile is B indices x 64 contraction indices of bf16.  Contraction contiguous (KM): B rows of 128 bytes,
-// 16-byte unit u of row r stored at u ^ (r & 7), so that the 16 rows of a fragment read touch all banks.
-// Contraction along the rows: 64 rows of 2B bytes, the 32-byte block b of row k stored at b ^ f(k),
-// f(k) = k[1:0] | k[3] << 2: the eight rows that a transposing read takes at a time lie in different banks.
+// A tile of an operand is B indices x 64 contraction indices of bf16, in panels of 64 rows of 128 bytes (8 KiB).
+// Contraction contiguous (KM): a panel is 64 indices; the 16-byte unit u of row r is stored at u ^ (r & 7), so that
+// the 16 rows of a fragment read touch all banks.  Contraction along the rows: a panel is 64 contraction indices of 64
+// neighbouring indices; the 32-byte block b of row k is stored at b ^ f(k), f(k) = k[1] | k[3] << 1: the eight rows
+// that half a wave's transposing read takes lie in different banks.  Eight lanes load a row: whole 128-byte lines.
 
-__device__ __forceinline__ int spread(int k) { return (k & 3) | ((k >> 1) & 4); }
+constexpr int kPanel = 64 * kBK * 2;
 
-template <int B, bool KM, int NT>
+__device__ __forceinline__ int spread(int k) { return ((k >> 1) & 1) | ((k >> 2) & 2); }
+
+// Sixteen bytes per lane from the buffer to LDS, lane after lane from the wave's address on.  Written in assembly, which
+// has no output register: the compiler puts a wait for all such loads in front of every transposing LDS read when it
+// knows of them, and would let none of them run ahead.  The waits are the caller's.
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, uint32_t offset) {
+    const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr)lds;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(rsrc) : "memory");
+}
+
+template <int B, bool KM, int NW>
 struct Operand {
-    static constexpr int kLoads = B * 8 / NT;
+    static constexpr int kLoads = B / 64 * 8 / NW;   // of 8 rows each, per wavefront
     static constexpr int kBytes = B * kBK * 2;
     uint32_t off[kLoads];
-    const uint16_t* base;     // of the current contraction step
+    const uint16_t* base;     // of the next contraction step to load
     int64_t step;             // elements per contraction step
+    int k0;                   // contraction index of the lane's first unit (KM: the same in every load)
 
-    // rows_of(r): the source row of tile row r relative to base, or -1 (contraction contiguous)
+    // rows_of(r): the source row of tile row r relative to base, or -1
     template <class F>
-    __device__ __forceinline__ void start_rows(const uint16_t* at, int64_t stride, F rows_of) {
+    __device__ __forceinline__ void start_rows(const uint16_t* at, int64_t stride, int wave, int lane, F rows_of) {
         static_assert(KM, "");
         base = at;
         step = kBK;
+        const int c = (lane & 7) ^ (lane >> 3);
+        k0 = c * 8;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int u = threadIdx.x + j * NT, r = u >> 3, c = (u & 7) ^ (r & 7);
-            const int src = rows_of(r);
+            const int src = rows_of((j * NW + wave) * 8 + (lane >> 3));
             off[j] = src < 0 ? kNowhere : (uint32_t)(src * stride * 2) + c * 16;
         }
     }
-    __device__ __forceinline__ void start_cols(const uint16_t* at, int64_t stride, int cols) {
+    __device__ __forceinline__ void start_cols(const uint16_t* at, int64_t stride, int wave, int lane, int cols) {
         static_assert(!KM, "");
         base = at;
         step = kBK * stride;
+        k0 = lane >> 3;
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int u = threadIdx.x + j * NT, k = u / (B / 8), c = (u % (B / 8)) ^ (spread(k) << 1);
-            off[j] = c * 8 < cols ? (uint32_t)(k * stride * 2) + c * 16 : kNowhere;
+            const int q = j * NW + wave, k = (q & 7) * 8 + (lane >> 3);
+            const int c = (q >> 3) * 64 + ((((lane >> 1) & 3) ^ spread(k)) * 2 + (lane & 1)) * 8;
+            off[j] = c < cols ? (uint32_t)((k * stride + c) * 2) : kNowhere;
         }
     }
-    // Loads the tile of the next contraction step; `left` = contraction indices that remain.
+    // Loads [j0, j1) of the tile of the current step; `left` = contraction indices that remain there.
+    template <int J0, int J1>
     __device__ __forceinline__ void load(char* lds, int left, int wave) {
         auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00027000);
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int u = threadIdx.x + j * NT;
-            const int k = KM ? (((u & 7) ^ ((u >> 3) & 7)) * 8) : u / (B / 8);
+        for (int j = J0; j < J1; ++j) {
+            const int k = KM ? k0 : k0 + ((j * NW + wave) & 7) * 8;
             const uint32_t o = k < left ? off[j] : kNowhere;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(lds + (j * NT + wave * 64) * 16), 16, o, 0, 0, 0);
+            load_to_lds(rsrc, lds + (j * NW + wave) * 1024, o);
         }
-        base += step;
     }
+    __device__ __forceinline__ void next() { base += step; }
 };
 
-// Fragment of 16 indices from `at` on and 32 contraction indices (half `ks` of the tile).
-template <int B, bool KM>
-__device__ __forceinline__ bf16x8 fragment(const char* lds, int at, int ks, int lane) {
+// What a lane adds to a tile's address to read its part of a fragment.
+template <bool KM>
+__device__ __forceinline__ uint32_t fragment_lane(int lane) {
+    if constexpr (KM) return (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+    const int k = (lane >> 4) * 8 + ((lane & 15) >> 2);
+    return k * 128 + spread(k) * 32 + (lane & 3) * 8;
+}
+
+// Fragment of the 16 indices from `at` (a multiple of 16) on and 32 contraction indices (half KS of the tile).
+template <bool KM, int KS>
+__device__ __forceinline__ bf16x8 fragment(const char* lds, int at, uint32_t mine) {
     if constexpr (KM) {
-        const int r = at + (lane & 15), c = ks * 4 + (lane >> 4);
-        return *(const bf16x8*)(lds + r * 128 + ((c ^ (r & 7)) << 4));
+        return *(const bf16x8*)(lds + at * 128 + (mine ^ (KS * 64)));
     } else {
-        const int k = ks * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
-        const int col = at + (lane & 3) * 4;
+        const char* p = lds + (at >> 6) * kPanel + KS * 32 * 128 + (mine ^ (((at >> 4) & 3) * 32));
         s16x4 v[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int kk = k + 4 * h;
-            const char* p = lds + kk * (B * 2) + (((col >> 3) ^ (spread(kk) << 1)) << 4) + (col & 7) * 2;
-            v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p);
-        }
+        for (int h = 0; h < 2; ++h) v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + h * 512));
         const s16x8 both = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(bf16x8, both);
     }
@@ -195,13 +212,20 @@ __device__ __forceinline__ void store4(uint16_t* p, const f32x4& v) {
     *(u32x2*)p = u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
 }
 
-template <int KIND, int BI, int BJ, int NWI, int NWJ>
-__global__ __launch_bounds__(64 * NWI * NWJ) void product_kernel(const Product a) {
-    constexpr int NT = 64 * NWI * NWJ;
+// A barrier that nothing is moved across; it waits for nobody's memory accesses.
+__device__ __forceinline__ void barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+template <int KIND, int BI, int BJ, int NWI, int NWJ, bool PHASED>
+__global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel(const Product a) {
     constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
     constexpr int WI = BI / NWI, WJ = BJ / NWJ, IT = WI / 16, JT = WJ / 16;
-    using P = Operand<BI, kPK, NT>;
-    using Q = Operand<BJ, kQK, NT>;
+    constexpr int NW = NWI * NWJ;
+    using P = Operand<BI, kPK, NW>;
+    using Q = Operand<BJ, kQK, NW>;
     constexpr int kStage = P::kBytes + Q::kBytes;
     constexpr int kLoads = P::kLoads + Q::kLoads;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -254,19 +278,19 @@ __global__ __launch_bounds__(64 * NWI * NWJ) void product_kernel(const Product a
         Q q;
         if constexpr (KIND == FORWARD) {
             const int I = a.I, gated = a.gated;
-            p.start_rows(a.p + e * a.p_expert + i0 * a.p_row, a.p_row, [=](int r) {
+            p.start_rows(a.p + e * a.p_expert + i0 * a.p_row, a.p_row, wave, lane, [=](int r) {
                 if (!gated) return i0 + r < I ? r : -1;
                 const int at = (r / WI) * (WI / 2) + r % (WI / 2);           // output column of the tile
                 return i0 + at < I ? at + ((r % WI) / (WI / 2)) * I : -1;    // second half of a wave's rows: up
             });
         } else if constexpr (KIND == GRAD_ROWS) {
-            p.start_cols(a.p + e * a.p_expert + i0, a.p_row, a.I - i0);
+            p.start_cols(a.p + e * a.p_expert + i0, a.p_row, wave, lane, a.I - i0);
         } else {
-            p.start_cols(a.p + e * a.p_expert + first * a.p_row + i0, a.p_row, a.I - i0);
+            p.start_cols(a.p + e * a.p_expert + first * a.p_row + i0, a.p_row, wave, lane, a.I - i0);
         }
         const uint16_t* qb = a.q + e * a.q_expert + first * a.q_row;
-        if constexpr (kQK) q.start_rows(qb + j0 * a.q_row, a.q_row, [=](int r) { return j0 + r < rows ? r : -1; });
-        else q.start_cols(qb + j0, a.q_row, a.J - j0);
+        if constexpr (kQK) q.start_rows(qb + j0 * a.q_row, a.q_row, wave, lane, [=](int r) { return j0 + r < rows ? r : -1; });
+        else q.start_cols(qb + j0, a.q_row, wave, lane, a.J - j0);
 
         f32x4 acc[IT][JT];
         f32x4 sums[JT];
@@ -279,43 +303,139 @@ __global__ __launch_bounds__(64 * NWI * NWJ) void product_kernel(const Product a
         const bool with_sums = KIND == GRAD_WEIGHTS && a.grad_b && ib == 0 && wi == 0;
 
         const int steps = (Kc + kBK - 1) / kBK;
-        if (steps) {
-            p.load(lds, Kc, wave);
-            q.load(lds + P::kBytes, Kc, wave);
-        }
-        for (int k = 0; k < steps; ++k) {
-            char* cur = lds + (k & 1) * kStage;
-            if (k + 1 < steps) {
-                char* nxt = lds + ((k + 1) & 1) * kStage;
-                p.load(nxt, Kc - (k + 1) * kBK, wave);
-                q.load(nxt + P::kBytes, Kc - (k + 1) * kBK, wave);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-            } else {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            }
-            __builtin_amdgcn_s_barrier();
-#pragma unroll
-            for (int ks = 0; ks < 2; ++ks) {
-                bf16x8 pf[IT], qf[JT];
-#pragma unroll
-                for (int it = 0; it < IT; ++it) pf[it] = fragment<BI, kPK>(cur, wi * WI + it * 16, ks, lane);
-#pragma unroll
-                for (int jt = 0; jt < JT; ++jt) qf[jt] = fragment<BJ, kQK>(cur + P::kBytes, wj * WJ + jt * 16, ks, lane);
-#pragma unroll
-                for (int it = 0; it < IT; ++it)
-#pragma unroll
-                    for (int jt = 0; jt < JT; ++jt)
-                        acc[it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[it], qf[jt], acc[it][jt], 0, 0, 0);
-                if (with_sums) {  // sums over the rows as a product with ones
-                    const s16x8 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
-#pragma unroll
-                    for (int jt = 0; jt < JT; ++jt)
-                        sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[jt], sums[jt], 0, 0, 0);
+        const uint32_t pl = fragment_lane<kPK>(lane), ql = fragment_lane<kQK>(lane);
+        const s16x8 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
+        if constexpr (PHASED) {
+            // Two groups of four wavefronts, one of each per SIMD, half a phase apart: while one group multiplies, the
+            // other reads fragments and issues loads.  A step has four phases, the quadrants of a wavefront's tile;
+            // each is a load interval and a product interval, and every interval ends in a barrier.  The part of the tile
+            // two steps ahead takes the place of what all wavefronts have finished reading: P's first half after
+            // phase 0, Q after phase 1, P's second half after phase 2.
+            static_assert(P::kLoads == 4 && Q::kLoads == 4 && NW == 8, "");
+            constexpr int IH = IT / 2, JH = JT / 2;
+            const bool late = wave >= 4;
+            if (steps) {
+                p.template load<0, 4>(lds, Kc, wave);
+                q.template load<0, 4>(lds + P::kBytes, Kc, wave);
+                p.next(); q.next();
+                if (steps > 1) {
+                    p.template load<0, 4>(lds + kStage, Kc - kBK, wave);
+                    q.template load<0, 4>(lds + kStage + P::kBytes, Kc - kBK, wave);
+                    p.next(); q.next();
+                    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 }
+                barrier();
+                if (late) barrier();
             }
-            // every wave has read the tile before anybody loads into its place
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
+            for (int k = 0; k < steps; ++k) {
+                char* cur = lds + (k & 1) * kStage;
+                const char* pc = cur + (wi * WI) * 128;
+                const char* qc = cur + P::kBytes + (wj * WJ) * 128;
+                const int left = Kc - (k + 2) * kBK;   // of the tile two steps ahead
+                const bool more = left > 0;
+                bf16x8 pf[2][IH], qf[2][JT];
+                auto read_p = [&](int half) {
+#pragma unroll
+                    for (int it = 0; it < IH; ++it) {
+                        pf[0][it] = fragment<kPK, 0>(pc, (half * IH + it) * 16, pl);
+                        pf[1][it] = fragment<kPK, 1>(pc, (half * IH + it) * 16, pl);
+                    }
+                };
+                auto read_q = [&](int half) {
+#pragma unroll
+                    for (int jt = 0; jt < JH; ++jt) {
+                        qf[0][half * JH + jt] = fragment<kQK, 0>(qc, (half * JH + jt) * 16, ql);
+                        qf[1][half * JH + jt] = fragment<kQK, 1>(qc, (half * JH + jt) * 16, ql);
+                    }
+                };
+                auto multiply = [&](int ih, int jh) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    barrier();
+                    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+                        for (int it = 0; it < IH; ++it)
+#pragma unroll
+                            for (int jt = 0; jt < JH; ++jt)
+                                acc[ih * IH + it][jh * JH + jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jh * JH + jt], acc[ih * IH + it][jh * JH + jt], 0, 0, 0);
+                        if (KIND == GRAD_WEIGHTS && ih == 0 && with_sums)  // sums over the rows as a product with ones
+#pragma unroll
+                            for (int jt = 0; jt < JH; ++jt)
+                                sums[jh * JH + jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jh * JH + jt], sums[jh * JH + jt], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_s_setprio(0);
+                    barrier();
+                };
+                read_p(0);
+                read_q(0);
+                multiply(0, 0);
+                read_q(1);
+                if (more) {
+                    p.template load<0, 1>(cur, left, wave);
+                    p.template load<2, 3>(cur, left, wave);
+                }
+                multiply(0, 1);
+                read_p(1);
+                if (more) q.template load<0, 4>(cur + P::kBytes, left, wave);
+                multiply(1, 1);
+                if (more) {
+                    p.template load<1, 2>(cur, left, wave);
+                    p.template load<3, 4>(cur, left, wave);
+                    p.next(); q.next();
+                    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next step's tile has landed
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                }
+                multiply(1, 0);
+            }
+            if (steps && !late) barrier();
+        } else {
+            if (steps) {
+                p.template load<0, P::kLoads>(lds, Kc, wave);
+                q.template load<0, Q::kLoads>(lds + P::kBytes, Kc, wave);
+            }
+            for (int k = 0; k < steps; ++k) {
+                const char* cur = lds + (k & 1) * kStage;
+                if (k + 1 < steps) {
+                    char* nxt = lds + ((k + 1) & 1) * kStage;
+                    p.next(); q.next();
+                    p.template load<0, P::kLoads>(nxt, Kc - (k + 1) * kBK, wave);
+                    q.template load<0, Q::kLoads>(nxt + P::kBytes, Kc - (k + 1) * kBK, wave);
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                }
+                barrier();
+                bf16x8 pf[2][IT], qf[2][JT];
+#pragma unroll
+                for (int it = 0; it < IT; ++it) {
+                    pf[0][it] = fragment<kPK, 0>(cur + wi * WI * 128, it * 16, pl);
+                    pf[1][it] = fragment<kPK, 1>(cur + wi * WI * 128, it * 16, pl);
+                }
+#pragma unroll
+                for (int jt = 0; jt < JT; ++jt) {
+                    qf[0][jt] = fragment<kQK, 0>(cur + P::kBytes + wj * WJ * 128, jt * 16, ql);
+                    qf[1][jt] = fragment<kQK, 1>(cur + P::kBytes + wj * WJ * 128, jt * 16, ql);
+                }
+#pragma unroll
+                for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+                    for (int it = 0; it < IT; ++it)
+#pragma unroll
+                        for (int jt = 0; jt < JT; ++jt)
+                            acc[it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jt], acc[it][jt], 0, 0, 0);
+                    if (with_sums)
+#pragma unroll
+                        for (int jt = 0; jt < JT; ++jt)
+                            sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jt], sums[jt], 0, 0, 0);
+                }
+                // every wavefront has read the tile before anybody loads into its place
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                barrier();
+            }
         }
 
         // Results: lane l holds, for index j = l % 16 of a fragment of Q, the indices i = 4 (l / 16) .. + 3 of one of P.
@@ -463,16 +583,15 @@ int64_t most_blocks(const Windows& w, int rows) {
 }
 
 template <int KIND>
-hipError_t launch(const Product& a, int64_t most_rows_blocks_128, hipStream_t s) {
-    constexpr int BI = 128, BJ = 128, NWI = 2, NWJ = 2;
+hipError_t launch(const Product& a, int64_t most_rows_blocks, hipStream_t s) {
+    constexpr int BI = 256, BJ = 256, NWI = 2, NWJ = 4;
     constexpr int lds = 2 * (BI + BJ) * kBK * 2 + (kMaxExperts + 1) * 4;
-    auto kernel = product_kernel<KIND, BI, BJ, NWI, NWJ>;
     const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
-    const int64_t most = most_rows_blocks_128 * ((a.I + bi - 1) / bi);
+    const int64_t most = most_rows_blocks * ((a.I + bi - 1) / bi);
     if (most <= 0) return hipSuccess;
     const int64_t cus = std::max(8, compute_units() / 8 * 8);
-    const int64_t grid = std::min(2 * cus, (most + 7) / 8 * 8);  // two workgroups fit a compute unit's LDS
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)grid), dim3(64 * NWI * NWJ), lds, s, a);
+    const int64_t grid = std::min(cus, (most + 7) / 8 * 8);
+    hipLaunchKernelGGL((product_kernel<KIND, BI, BJ, NWI, NWJ, true>), dim3((uint32_t)grid), dim3(64 * NWI * NWJ), lds, s, a);
     return hipGetLastError();
 }
 
@@ -500,7 +619,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     p.pre = a.pre.base; p.pre_expert = a.pre.expert_stride; p.pre_row = a.pre.row_stride;
     p.res = a.res.base; p.res_expert = a.res.expert_stride; p.res_row = a.res.row_stride;
     p.status = a.status;
-    return launch<FORWARD>(p, most_blocks(a.win, 128), s);
+    return launch<FORWARD>(p, most_blocks(a.win, 256), s);
 }
 
 hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
@@ -510,7 +629,7 @@ hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
     p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
     p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
     p.I = a.Kd; p.Kc = a.N;
-    return launch<GRAD_ROWS>(p, most_blocks(a.win, 128), s);
+    return launch<GRAD_ROWS>(p, most_blocks(a.win, 256), s);
 }
 
 hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
@@ -522,7 +641,7 @@ hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
     p.out_f32 = a.gw_f32; p.accumulate = a.accumulate;
     p.grad_b = a.grad_b; p.gb_stride = a.gb_stride;
     p.I = a.Kd; p.J = a.N;
-    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + 127) / 128), s);
+    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + 255) / 256), s);
 }
 
 hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s) {
