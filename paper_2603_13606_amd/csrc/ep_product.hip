@@ -307,22 +307,24 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
         const s16x8 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
         if constexpr (PHASED) {
             // Two groups of four wavefronts, one of each per SIMD, half a phase apart: while one group multiplies, the
-            // other reads fragments and issues loads.  A step has four phases, the quadrants of a wavefront's tile;
-            // each is a load interval and a product interval, and every interval ends in a barrier.  The part of the tile
-            // two steps ahead takes the place of what all wavefronts have finished reading: P's first half after
-            // phase 0, Q after phase 1, P's second half after phase 2.
+            // other reads fragments and issues loads.  A step has two phases, the halves of a wavefront's tile along P;
+            // each is a load interval and a product interval of 32 instructions, and every interval ends in a barrier.
+            // The tile two steps ahead takes the place of what all wavefronts have finished reading: P's first half and
+            // Q after phase 0, P's second half after phase 1.  So six loads are issued in phase 1 of step k for step
+            // k + 2 and two in phase 0 of step k + 1, and in both places waiting for all but the youngest eight leaves
+            // what the next phase reads in LDS.
             static_assert(P::kLoads == 4 && Q::kLoads == 4 && NW == 8, "");
-            constexpr int IH = IT / 2, JH = JT / 2;
+            constexpr int IH = IT / 2;
             const bool late = wave >= 4;
             if (steps) {
                 p.template load<0, 4>(lds, Kc, wave);
                 q.template load<0, 4>(lds + P::kBytes, Kc, wave);
                 p.next(); q.next();
                 if (steps > 1) {
-                    p.template load<0, 4>(lds + kStage, Kc - kBK, wave);
+                    p.template load<0, 1>(lds + kStage, Kc - kBK, wave);
+                    p.template load<2, 3>(lds + kStage, Kc - kBK, wave);
                     q.template load<0, 4>(lds + kStage + P::kBytes, Kc - kBK, wave);
-                    p.next(); q.next();
-                    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                    asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
                 } else {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 }
@@ -331,10 +333,9 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
             }
             for (int k = 0; k < steps; ++k) {
                 char* cur = lds + (k & 1) * kStage;
+                char* nxt = lds + ((k + 1) & 1) * kStage;
                 const char* pc = cur + (wi * WI) * 128;
                 const char* qc = cur + P::kBytes + (wj * WJ) * 128;
-                const int left = Kc - (k + 2) * kBK;   // of the tile two steps ahead
-                const bool more = left > 0;
                 bf16x8 pf[2][IH], qf[2][JT];
                 auto read_p = [&](int half) {
 #pragma unroll
@@ -343,14 +344,7 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
                         pf[1][it] = fragment<kPK, 1>(pc, (half * IH + it) * 16, pl);
                     }
                 };
-                auto read_q = [&](int half) {
-#pragma unroll
-                    for (int jt = 0; jt < JH; ++jt) {
-                        qf[0][half * JH + jt] = fragment<kQK, 0>(qc, (half * JH + jt) * 16, ql);
-                        qf[1][half * JH + jt] = fragment<kQK, 1>(qc, (half * JH + jt) * 16, ql);
-                    }
-                };
-                auto multiply = [&](int ih, int jh) {
+                auto multiply = [&](int ih) {
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     barrier();
                     __builtin_amdgcn_s_setprio(1);
@@ -359,37 +353,41 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
 #pragma unroll
                         for (int it = 0; it < IH; ++it)
 #pragma unroll
-                            for (int jt = 0; jt < JH; ++jt)
-                                acc[ih * IH + it][jh * JH + jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jh * JH + jt], acc[ih * IH + it][jh * JH + jt], 0, 0, 0);
+                            for (int jt = 0; jt < JT; ++jt)
+                                acc[ih * IH + it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jt], acc[ih * IH + it][jt], 0, 0, 0);
                         if (KIND == GRAD_WEIGHTS && ih == 0 && with_sums)  // sums over the rows as a product with ones
 #pragma unroll
-                            for (int jt = 0; jt < JH; ++jt)
-                                sums[jh * JH + jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jh * JH + jt], sums[jh * JH + jt], 0, 0, 0);
+                            for (int jt = 0; jt < JT; ++jt)
+                                sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jt], sums[jt], 0, 0, 0);
                     }
                     __builtin_amdgcn_s_setprio(0);
                     barrier();
                 };
                 read_p(0);
-                read_q(0);
-                multiply(0, 0);
-                read_q(1);
-                if (more) {
-                    p.template load<0, 1>(cur, left, wave);
-                    p.template load<2, 3>(cur, left, wave);
+#pragma unroll
+                for (int jt = 0; jt < JT; ++jt) {
+                    qf[0][jt] = fragment<kQK, 0>(qc, jt * 16, ql);
+                    qf[1][jt] = fragment<kQK, 1>(qc, jt * 16, ql);
                 }
-                multiply(0, 1);
-                read_p(1);
-                if (more) q.template load<0, 4>(cur + P::kBytes, left, wave);
-                multiply(1, 1);
-                if (more) {
-                    p.template load<1, 2>(cur, left, wave);
-                    p.template load<3, 4>(cur, left, wave);
+                if (k + 1 < steps) {
+                    p.template load<1, 2>(nxt, Kc - (k + 1) * kBK, wave);
+                    p.template load<3, 4>(nxt, Kc - (k + 1) * kBK, wave);
                     p.next(); q.next();
-                    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");   // the next step's tile has landed
+                    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
                 } else {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 }
-                multiply(1, 0);
+                multiply(0);
+                read_p(1);
+                if (k + 2 < steps) {
+                    p.template load<0, 1>(cur, Kc - (k + 2) * kBK, wave);
+                    p.template load<2, 3>(cur, Kc - (k + 2) * kBK, wave);
+                    q.template load<0, 4>(cur + P::kBytes, Kc - (k + 2) * kBK, wave);
+                    asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(2)" ::: "memory");
+                }
+                multiply(1);
             }
             if (steps && !late) barrier();
         } else {
