@@ -679,8 +679,8 @@ EP_API ep_result_t ep_expert_product(ep_handle_t handle, const ep_product_config
  * outputs: PREACT grad_pre, rows of N bf16 (given exactly when pre is; may be pre itself): the gradient of
  *          pre, which the other two products read;
  *          TOKENS grad_x = grad_pre W_e (optional; may be neither g nor grad_pre);
- *          EXPERT_WEIGHTS grad_W_e = grad_pre^T x, [L, N, Kd] f32 or bf16 (optional), zeros for an expert
- *          without rows; EXPERT_BIAS [L, N], of the same type, column sums of grad_pre (optional, only
+ *          EXPERT_WEIGHTS grad_W_e = grad_pre^T x, [L, N, Kd] f32 (rows less than 2^21 elements apart) or bf16
+ *          (optional), zeros for an expert without rows; EXPERT_BIAS [L, N], of the same type, column sums of grad_pre (optional, only
  *          with grad_W).
  * Sums in float32, over the rows in one fixed order.  At least one of W and grad_W is given.
  * Errors: EP_ERR_INVALID_ARG, EP_ERR_HIP.

@@ -52,6 +52,7 @@ bool check_weights(const ep_tensor_t* t, bool f32_too = false) {
     if (t->shape[1] < 8 || t->shape[1] % 8 || t->shape[1] > kMaxExtent || t->shape[2] < 8 || t->shape[2] % 8 || t->shape[2] > kMaxExtent)
         return false;
     if (t->stride[2] != 1 || t->stride[1] < t->shape[2] || t->stride[1] % 8 || t->stride[1] >= kMaxExtent) return false;
+    if (t->dtype == EP_DTYPE_F32 && t->stride[1] >= kMaxExtent / 2) return false;
     return t->stride[0] % 8 == 0 && t->stride[0] >= 0;
 }
 

@@ -25,10 +25,11 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kBK = 64;                       // contraction indices per LDS tile
-constexpr uint32_t kNowhere = 0x80000000u;    // offset of a lane that has nothing to load: beyond the buffer's end, gives zeros
+constexpr uint32_t kNowhere = 0x80000000u;    // offset of a lane that has nothing there: beyond the buffer's end, reads zeros
 
 enum { FORWARD = 0, GRAD_ROWS = 1, GRAD_WEIGHTS = 2 };
 
@@ -64,9 +65,15 @@ __device__ __forceinline__ int window_rows(const Windows& w, int e, int64_t* fir
     return (int)n;
 }
 
-// starts[e] = blocks of `rows` rows before expert e, starts[L] = all of them; one wavefront.  Returns
-// whether a window reaches beyond its tensor.
-__device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, int* starts, int lane) {
+// The windows of a call in LDS: first row and rows of each expert, starts[e] = blocks of `rows` rows before expert e,
+// starts[L] = all of them.
+struct Table {
+    int starts[kMaxExperts + 1], first[kMaxExperts], rows[kMaxExperts];
+};
+
+// By one wavefront.  Returns whether a window reaches beyond its tensor.
+__device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, Table* table, int lane) {
+    int* starts = table->starts;
     const int per = (w.L + 63) / 64;
     const int e0 = lane * per, e1 = min(w.L, e0 + per);
     int sum = 0;
@@ -75,6 +82,8 @@ __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, int* sta
         int64_t at;
         const int n = window_rows(w, e, &at);
         cut |= n < w.count[e];
+        table->first[e] = (int)at;
+        table->rows[e] = n;
         sum += (n + rows - 1) / rows;
     }
     int before = sum;
@@ -85,9 +94,8 @@ __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, int* sta
     }
     int at = before - sum;
     for (int e = e0; e < e1; ++e) {
-        int64_t first;
         starts[e] = at;
-        at += (window_rows(w, e, &first) + rows - 1) / rows;
+        at += (table->rows[e] + rows - 1) / rows;
     }
     if (lane == 63) starts[w.L] = before;
     return __any(cut);
@@ -196,20 +204,33 @@ __device__ __forceinline__ bf16x8 fragment(const char* lds, int at, uint32_t min
     }
 }
 
-__device__ __forceinline__ f32x4 load4(const void* p, int64_t i, int is_f32) {
-    f32x4 v;
-    if (is_f32) {
-        v = *(const f32x4*)((const float*)p + i);
-    } else {
-        const u32x2 u = *(const u32x2*)((const uint16_t*)p + i);
-        v = f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16),
-                  __uint_as_float(u[1] & 0xffff0000u)};
-    }
+__device__ __forceinline__ f32x4 widen(const u32x2& u) {
+    return f32x4{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xffff0000u), __uint_as_float(u[1] << 16),
+                 __uint_as_float(u[1] & 0xffff0000u)};
+}
+
+// Keeps what is computed from v inside the loop over the tiles: lifted out of it, it would hold registers all along.
+__device__ __forceinline__ int opaque(int v) {
+    asm volatile("" : "+v"(v));
     return v;
 }
 
-__device__ __forceinline__ void store4(uint16_t* p, const f32x4& v) {
-    *(u32x2*)p = u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+// Accesses of results: a lane that has nothing there reads zeros and writes nothing (offset kNowhere).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t results(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00027000);
+}
+__device__ __forceinline__ f32x4 load4(__amdgpu_buffer_rsrc_t r, uint32_t off, int is_f32) {
+    if (is_f32) return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+    return widen(__builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0)));
+}
+
+// Four values each of two neighbouring fragments of P, for one index of Q, as bf16: the lanes of two neighbouring rows of
+// 16 exchange halves, so that each writes eight values of one fragment, 16 bytes; four lanes write 64 in a row.
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, uint32_t off, const f32x4& v, const f32x4& w) {
+    const auto lo = __builtin_amdgcn_permlane16_swap(pack2_bf16(v[0], v[1]), pack2_bf16(w[0], w[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(pack2_bf16(v[2], v[3]), pack2_bf16(w[2], w[3]), false, false);
+    const u32x4 u = {lo[0], hi[0], lo[1], hi[1]};
+    __builtin_amdgcn_raw_buffer_store_b128(u, r, off, 0, 0);
 }
 
 // A barrier that nothing is moved across; it waits for nobody's memory accesses.
@@ -229,7 +250,7 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
     constexpr int kStage = P::kBytes + Q::kBytes;
     constexpr int kLoads = P::kLoads + Q::kLoads;
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    int* starts = (int*)(lds + 2 * kStage);
+    Table* table = (Table*)(lds + 2 * kStage);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave % NWI, wj = wave / NWI;
 
@@ -237,61 +258,82 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
     // times blocks along I.  A gated tile holds BI/2 outputs: their gate and their up columns.
     const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
     const int ni = (a.I + bi - 1) / bi;
-    int nj;
-    if (KIND == GRAD_WEIGHTS) {
-        nj = a.win.L * ((a.J + BJ - 1) / BJ);
-    } else {
-        if (wave == 0) {
-            const bool cut = scan_blocks(a.win, BJ, starts, lane);
-            if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && lane == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
-        }
-        __syncthreads();
-        nj = __builtin_amdgcn_readfirstlane(starts[a.win.L]);
+    if (wave == 0) {
+        const bool cut = scan_blocks(a.win, BJ, table, lane);
+        if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && lane == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
     }
+    __syncthreads();
+    const int weight_blocks = KIND == GRAD_WEIGHTS ? (a.J + BJ - 1) / BJ : 0;
+    const int nj = KIND == GRAD_WEIGHTS ? a.win.L * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[a.win.L]);
     const int64_t tiles = (int64_t)nj * ni;
 
-    // Workgroups of one XCD (blockIdx mod 8) take neighbouring tiles, eight row blocks by a few column
-    // blocks, so that its L2 serves both operands.
-    const int per = gridDim.x >> 3;
-    for (int64_t t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3); t < tiles; t += gridDim.x) {
-        const int64_t band = t / (8 * (int64_t)ni);
-        const int height = (int)min((int64_t)8, nj - band * 8);
-        const int in = (int)(t - band * 8 * ni);
-        const int jb = __builtin_amdgcn_readfirstlane((int)(band * 8) + in % height);
+    // Tile t: expert by expert, within an expert in bands of eight row blocks, within a band column block by column block.
+    // Workgroups of one XCD (blockIdx mod 8) take neighbouring tiles, so that its L2 serves both operands.
+    struct Tile {
+        int e, i0, j0, rows, first;
+        bool first_i;
+    };
+    auto locate = [&](int64_t t) {
+        Tile c;
+        const int block = (int)(t / ni);
+        c.e = __builtin_amdgcn_readfirstlane(KIND == GRAD_WEIGHTS ? block / weight_blocks : find_expert(table->starts, a.win.L, block));
+        const int start = KIND == GRAD_WEIGHTS ? c.e * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[c.e]);
+        const int m = (KIND == GRAD_WEIGHTS ? (c.e + 1) * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[c.e + 1])) - start;
+        const int64_t local = t - (int64_t)start * ni;
+        const int band = (int)(local / (8 * ni)), height = min(8, m - band * 8), in = (int)(local - (int64_t)band * 8 * ni);
         const int ib = __builtin_amdgcn_readfirstlane(in / height);
-        int e, j0;
-        if (KIND == GRAD_WEIGHTS) {
-            const int per_expert = (a.J + BJ - 1) / BJ;
-            e = jb / per_expert;
-            j0 = (jb - e * per_expert) * BJ;
-        } else {
-            e = __builtin_amdgcn_readfirstlane(find_expert(starts, a.win.L, jb));
-            j0 = (jb - __builtin_amdgcn_readfirstlane(starts[e])) * BJ;
-        }
-        int64_t first;
-        const int rows = window_rows(a.win, e, &first);
-        const int i0 = ib * bi;
-        const int Kc = KIND == GRAD_WEIGHTS ? rows : a.Kc;
-        const int J = KIND == GRAD_WEIGHTS ? a.J : rows;
-
-        P p;
-        Q q;
+        c.j0 = __builtin_amdgcn_readfirstlane(band * 8 + in - ib * height) * BJ;
+        c.i0 = ib * bi;
+        c.first_i = ib == 0;
+        c.rows = __builtin_amdgcn_readfirstlane(table->rows[c.e]);
+        c.first = __builtin_amdgcn_readfirstlane(table->first[c.e]);
+        return c;
+    };
+    P p;
+    Q q;
+    auto steps_of = [&](const Tile& c) { return ((KIND == GRAD_WEIGHTS ? c.rows : a.Kc) + kBK - 1) / kBK; };
+    // Points the operands at a tile and issues its first loads: all of step 0, and of step 1 what its phase 0 reads.
+    auto begin = [&](const Tile& c) {
+        const int lane = opaque(threadIdx.x & 63);
+        const uint16_t* pb = a.p + c.e * a.p_expert;
         if constexpr (KIND == FORWARD) {
-            const int I = a.I, gated = a.gated;
-            p.start_rows(a.p + e * a.p_expert + i0 * a.p_row, a.p_row, wave, lane, [=](int r) {
+            const int I = a.I, gated = a.gated, i0 = c.i0;
+            p.start_rows(pb + c.i0 * a.p_row, a.p_row, wave, lane, [=](int r) {
                 if (!gated) return i0 + r < I ? r : -1;
                 const int at = (r / WI) * (WI / 2) + r % (WI / 2);           // output column of the tile
                 return i0 + at < I ? at + ((r % WI) / (WI / 2)) * I : -1;    // second half of a wave's rows: up
             });
         } else if constexpr (KIND == GRAD_ROWS) {
-            p.start_cols(a.p + e * a.p_expert + i0, a.p_row, wave, lane, a.I - i0);
+            p.start_cols(pb + c.i0, a.p_row, wave, lane, a.I - c.i0);
         } else {
-            p.start_cols(a.p + e * a.p_expert + first * a.p_row + i0, a.p_row, wave, lane, a.I - i0);
+            p.start_cols(pb + c.first * a.p_row + c.i0, a.p_row, wave, lane, a.I - c.i0);
         }
-        const uint16_t* qb = a.q + e * a.q_expert + first * a.q_row;
-        if constexpr (kQK) q.start_rows(qb + j0 * a.q_row, a.q_row, wave, lane, [=](int r) { return j0 + r < rows ? r : -1; });
-        else q.start_cols(qb + j0, a.q_row, wave, lane, a.J - j0);
+        const uint16_t* qb = a.q + c.e * a.q_expert + c.first * a.q_row;
+        const int rows_left = c.rows - c.j0;
+        if constexpr (kQK) q.start_rows(qb + c.j0 * a.q_row, a.q_row, wave, lane, [=](int r) { return r < rows_left ? r : -1; });
+        else q.start_cols(qb + c.j0, a.q_row, wave, lane, a.J - c.j0);
+        const int Kc = KIND == GRAD_WEIGHTS ? c.rows : a.Kc;
+        if (Kc > 0) {
+            p.template load<0, P::kLoads>(lds, Kc, wave);
+            q.template load<0, Q::kLoads>(lds + P::kBytes, Kc, wave);
+            p.next(); q.next();
+            if (PHASED && Kc > kBK) {
+                p.template load<0, 1>(lds + kStage, Kc - kBK, wave);
+                p.template load<2, 3>(lds + kStage, Kc - kBK, wave);
+                q.template load<0, 4>(lds + kStage + P::kBytes, Kc - kBK, wave);
+            }
+        }
+    };
 
+    const int per = gridDim.x >> 3;
+    int64_t t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (t >= tiles) return;
+    Tile c = locate(t);
+    begin(c);
+    bool fresh = true;   // no results have been stored since the tile's first loads
+    for (;;) {
+        const int steps = steps_of(c);
+        const int Kc = KIND == GRAD_WEIGHTS ? c.rows : a.Kc;
         f32x4 acc[IT][JT];
         f32x4 sums[JT];
 #pragma unroll
@@ -300,9 +342,8 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
 #pragma unroll
             for (int it = 0; it < IT; ++it) acc[it][jt] = f32x4{0, 0, 0, 0};
         }
-        const bool with_sums = KIND == GRAD_WEIGHTS && a.grad_b && ib == 0 && wi == 0;
+        const bool with_sums = KIND == GRAD_WEIGHTS && a.grad_b && c.first_i && wi == 0;
 
-        const int steps = (Kc + kBK - 1) / kBK;
         const uint32_t pl = fragment_lane<kPK>(lane), ql = fragment_lane<kQK>(lane);
         const s16x8 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
         if constexpr (PHASED) {
@@ -317,16 +358,16 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
             constexpr int IH = IT / 2;
             const bool late = wave >= 4;
             if (steps) {
-                p.template load<0, 4>(lds, Kc, wave);
-                q.template load<0, 4>(lds + P::kBytes, Kc, wave);
-                p.next(); q.next();
-                if (steps > 1) {
-                    p.template load<0, 1>(lds + kStage, Kc - kBK, wave);
-                    p.template load<2, 3>(lds + kStage, Kc - kBK, wave);
-                    q.template load<0, 4>(lds + kStage + P::kBytes, Kc - kBK, wave);
-                    asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
-                } else {
+                // Step 0 has landed when only the six loads for step 1 and the results stored since are on their way: of
+                // those at least 8 (gated) or 16 per lane.
+                if (steps == 1) {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                } else if (fresh) {
+                    asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+                } else if (KIND == FORWARD && a.gated) {
+                    asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
+                } else {
+                    asm volatile("s_waitcnt vmcnt(22)" ::: "memory");
                 }
                 barrier();
                 if (late) barrier();
@@ -391,17 +432,13 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
             }
             if (steps && !late) barrier();
         } else {
-            if (steps) {
-                p.template load<0, P::kLoads>(lds, Kc, wave);
-                q.template load<0, Q::kLoads>(lds + P::kBytes, Kc, wave);
-            }
             for (int k = 0; k < steps; ++k) {
                 const char* cur = lds + (k & 1) * kStage;
                 if (k + 1 < steps) {
                     char* nxt = lds + ((k + 1) & 1) * kStage;
-                    p.next(); q.next();
                     p.template load<0, P::kLoads>(nxt, Kc - (k + 1) * kBK, wave);
                     q.template load<0, Q::kLoads>(nxt + P::kBytes, Kc - (k + 1) * kBK, wave);
+                    p.next(); q.next();
                     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
                 } else {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -436,95 +473,139 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
             }
         }
 
-        // Results: lane l holds, for index j = l % 16 of a fragment of Q, the indices i = 4 (l / 16) .. + 3 of one of P.
-        const int jl = lane & 15, il = (lane >> 4) * 4;
+        // The next tile's first loads run while this one's results are written.
+        const Tile done = c;
+        const int64_t next = t + gridDim.x;
+        const bool again = next < tiles;
+        if (again) {
+            c = locate(next);
+            begin(c);
+        }
+
+        // Results: lane l holds, for index j = l % 16 of a fragment of Q, the indices i = 4 (l / 16) .. + 3 of one of P;
+        // stored in pairs of fragments (store8), eight of one: i8.
+        const int mine = opaque(threadIdx.x & 63), g = mine >> 4;
+        const int J = (KIND == GRAD_WEIGHTS ? a.J : done.rows) - done.j0;
+        const int iw = wi * (KIND == FORWARD && a.gated ? WI / 2 : WI), jw = wj * WJ + (mine & 15);
+        const int i4 = iw + g * 4, i8 = iw + (g & 1) * 16 + (g >> 1) * 8;
+        const int Il = a.I - done.i0;   // columns of the tile that there are
+        const int esize = KIND == GRAD_WEIGHTS && a.out_f32 ? 4 : 2;
+        // Byte offset of (index j of fragment jt, column i) in a matrix whose rows are `row` elements apart.
+        auto at = [&](int jt, int i, int64_t row, int size) {
+            const int j = jw + jt * 16;
+            return (j < J ? (uint32_t)(j * row * size) : kNowhere) + (i < Il ? (uint32_t)(i * size) : kNowhere - 1);
+        };
+        const char* out = (const char*)a.out;
+        if constexpr (KIND == GRAD_WEIGHTS) out += (done.e * a.out_expert + done.j0 * a.out_row + done.i0) * esize;
+        else out += (done.e * a.out_expert + (done.first + done.j0) * a.out_row + done.i0) * 2;
+        const auto ro = results(out);
         if constexpr (KIND == FORWARD) {
-            const int64_t ob = e * a.out_expert + first * a.out_row, pb = e * a.pre_expert + first * a.pre_row,
-                          rb = e * a.res_expert + first * a.res_row;
-            const char* bias = a.bias ? (const char*)a.bias + e * a.bias_stride * (a.bias_f32 ? 4 : 2) : nullptr;
             const int nit = a.gated ? IT / 2 : IT;
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                if (it >= nit) continue;
-                const int i = i0 + wi * (a.gated ? WI / 2 : WI) + it * 16 + il;
-                if (i >= a.I) continue;
-                f32x4 b = {0, 0, 0, 0}, bu = {0, 0, 0, 0};
-                if (bias) {
-                    b = load4(bias, i, a.bias_f32);
-                    if (a.gated) bu = load4(bias, i + a.I, a.bias_f32);
-                }
-#pragma unroll
-                for (int jt = 0; jt < JT; ++jt) {
-                    const int j = j0 + wj * WJ + jt * 16 + jl;
-                    if (j >= J) continue;
-                    f32x4 v, up;
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = acc[it][jt][r] + b[r];
-                    if (a.gated) {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) up[r] = acc[(it + IT / 2) % IT][jt][r] + bu[r];
-                    }
-                    if (a.pre) {
-                        uint16_t* at = a.pre + pb + j * a.pre_row + i;
-                        store4(at, v);
-                        if (a.gated) store4(at + a.I, up);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        v[r] = activate(a.act, v[r]);
-                        if (a.gated) v[r] *= up[r];
-                    }
-                    if (a.res) {
-                        const f32x4 res = load4(a.res + rb + j * a.res_row, i, 0);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) v[r] += res[r];
-                    }
-                    store4(a.out + ob + j * a.out_row + i, v);
-                }
-            }
-        } else if constexpr (KIND == GRAD_ROWS) {
-            const int64_t ob = e * a.out_expert + first * a.out_row;
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = i0 + wi * WI + it * 16 + il;
-                if (i >= a.I) continue;
-#pragma unroll
-                for (int jt = 0; jt < JT; ++jt) {
-                    const int j = j0 + wj * WJ + jt * 16 + jl;
-                    if (j < J) store4(a.out + ob + j * a.out_row + i, acc[it][jt]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) {
-                const int j = j0 + wj * WJ + jt * 16 + jl;
-                if (j >= J) continue;
-                if (with_sums && il == 0) {
-                    const int64_t at = e * a.gb_stride + j;
-                    if (a.out_f32) {
-                        float* g = (float*)a.grad_b + at;
-                        *g = a.accumulate ? *g + sums[jt][0] : sums[jt][0];
-                    } else {
-                        uint16_t* g = (uint16_t*)a.grad_b + at;
-                        *g = (uint16_t)pack2_bf16(a.accumulate ? bf16_f32(*g) + sums[jt][0] : sums[jt][0], 0.0f);
-                    }
-                }
+            if (a.bias) {
+                const int size = a.bias_f32 ? 4 : 2;
+                const auto rb = results((const char*)a.bias + (done.e * a.bias_stride + done.i0) * size);
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
-                    const int i = i0 + wi * WI + it * 16 + il;
-                    if (i >= a.I) continue;
-                    const int64_t at = e * a.out_expert + j * a.out_row + i;
-                    f32x4 v = acc[it][jt];
-                    if (a.accumulate) {
-                        const f32x4 old = load4(a.out, at, a.out_f32);
+                    const int i = i4 + (it < nit ? it : it - nit) * 16;
+                    const f32x4 b = load4(rb, i < Il ? (uint32_t)((it < nit ? i : i + a.I) * size) : kNowhere, a.bias_f32);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) v[r] += old[r];
-                    }
-                    if (a.out_f32) *(f32x4*)((float*)a.out + at) = v;
-                    else store4(a.out + at, v);
+                    for (int jt = 0; jt < JT; ++jt)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[it][jt][r] += b[r];
                 }
             }
+            if (a.pre) {
+                const auto rp = results(a.pre + done.e * a.pre_expert + (done.first + done.j0) * a.pre_row + done.i0);
+#pragma unroll
+                for (int it = 0; it < IT; it += 2)
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt) {
+                        const int i = i8 + (it < nit ? it : it - nit) * 16;
+                        store8(rp, at(jt, i, a.pre_row, 2) + (it < nit || i >= Il ? 0 : a.I * 2), acc[it][jt], acc[it + 1][jt]);
+                    }
+            }
+            const auto rr = results(a.res + done.e * a.res_expert + (done.first + done.j0) * a.res_row + done.i0);
+            auto finish = [&](auto activation, auto gate) {
+                constexpr int kN = decltype(gate)::value ? IT / 2 : IT;
+#pragma unroll
+                for (int it = 0; it < kN; it += 2)
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt) {
+                        f32x4 v[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                v[h][r] = activate(decltype(activation)::value, acc[it + h][jt][r]);
+                                if (decltype(gate)::value) v[h][r] *= acc[(it + h + IT / 2) % IT][jt][r];
+                            }
+                            if (a.res) {
+                                const f32x4 res = load4(rr, at(jt, i4 + (it + h) * 16, a.res_row, 2), 0);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) v[h][r] += res[r];
+                            }
+                        }
+                        store8(ro, at(jt, i8 + it * 16, a.out_row, 2), v[0], v[1]);
+                    }
+            };
+            auto with = [&](auto activation) {
+                if (a.gated) finish(activation, std::true_type());
+                else finish(activation, std::false_type());
+            };
+            if (a.act == EP_ACT_SILU) with(std::integral_constant<int, EP_ACT_SILU>());
+            else if (a.act == EP_ACT_GELU) with(std::integral_constant<int, EP_ACT_GELU>());
+            else with(std::integral_constant<int, EP_ACT_NONE>());
+        } else {
+            if (KIND == GRAD_WEIGHTS && with_sums && g == 0) {
+#pragma unroll
+                for (int jt = 0; jt < JT; ++jt) {
+                    if (jw + jt * 16 >= J) continue;
+                    const int64_t to = done.e * a.gb_stride + done.j0 + jw + jt * 16;
+                    if (a.out_f32) {
+                        float* b = (float*)a.grad_b + to;
+                        *b = a.accumulate ? *b + sums[jt][0] : sums[jt][0];
+                    } else {
+                        uint16_t* b = (uint16_t*)a.grad_b + to;
+                        *b = (uint16_t)pack2_bf16(a.accumulate ? bf16_f32(*b) + sums[jt][0] : sums[jt][0], 0.0f);
+                    }
+                }
+            }
+            auto finish = [&](auto wide, auto accumulate) {
+                constexpr int kSize = decltype(wide)::value ? 4 : 2;
+#pragma unroll
+                for (int it = 0; it < IT; it += 2)
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt) {
+                        f32x4 v[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            v[h] = acc[it + h][jt];
+                            const uint32_t to = at(jt, i4 + (it + h) * 16, a.out_row, kSize);
+                            if (decltype(accumulate)::value) {
+                                const f32x4 old = load4(ro, to, kSize == 4);
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) v[h][r] += old[r];
+                            }
+                            if (kSize == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v[h]), ro, to, 0, 0);
+                        }
+                        if (kSize == 2) store8(ro, at(jt, i8 + it * 16, a.out_row, 2), v[0], v[1]);
+                    }
+            };
+            if constexpr (KIND == GRAD_WEIGHTS) {
+                if (a.out_f32) {
+                    if (a.accumulate) finish(std::true_type(), std::true_type());
+                    else finish(std::true_type(), std::false_type());
+                } else {
+                    if (a.accumulate) finish(std::false_type(), std::true_type());
+                    else finish(std::false_type(), std::false_type());
+                }
+            } else {
+                finish(std::false_type(), std::false_type());
+            }
         }
+        if (!again) return;
+        t = next;
+        fresh = false;
     }
 }
 
@@ -545,14 +626,14 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
 }
 
 __global__ __launch_bounds__(256) void act_backward_kernel(const ActBackwardArgs a) {
-    __shared__ int starts[kMaxExperts + 1];
-    if (threadIdx.x < 64) scan_blocks(a.win, kActRows, starts, threadIdx.x);
+    __shared__ Table table;
+    if (threadIdx.x < 64) scan_blocks(a.win, kActRows, &table, threadIdx.x);
     __syncthreads();
     const int units = a.No / 8;
-    for (int b = blockIdx.x; b < starts[a.win.L]; b += gridDim.x) {
-        const int e = find_expert(starts, a.win.L, b);
-        int64_t first;
-        const int rows = window_rows(a.win, e, &first), r0 = (b - starts[e]) * kActRows, n = min(kActRows, rows - r0);
+    for (int b = blockIdx.x; b < table.starts[a.win.L]; b += gridDim.x) {
+        const int e = find_expert(table.starts, a.win.L, b);
+        const int64_t first = table.first[e];
+        const int r0 = (b - table.starts[e]) * kActRows, n = min(kActRows, table.rows[e] - r0);
         for (int i = threadIdx.x; i < n * units; i += 256) {
             const int r = r0 + i / units, c = (i % units) * 8;
             const uint16_t* pre = a.pre.base + e * a.pre.expert_stride + (first + r) * a.pre.row_stride + c;
@@ -583,7 +664,7 @@ int64_t most_blocks(const Windows& w, int rows) {
 template <int KIND>
 hipError_t launch(const Product& a, int64_t most_rows_blocks, hipStream_t s) {
     constexpr int BI = 256, BJ = 256, NWI = 2, NWJ = 4;
-    constexpr int lds = 2 * (BI + BJ) * kBK * 2 + (kMaxExperts + 1) * 4;
+    constexpr int lds = 2 * (BI + BJ) * kBK * 2 + (int)sizeof(Table);
     const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
     const int64_t most = most_rows_blocks * ((a.I + bi - 1) / bi);
     if (most <= 0) return hipSuccess;
