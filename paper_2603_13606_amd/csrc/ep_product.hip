@@ -240,17 +240,30 @@ __device__ __forceinline__ void barrier() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int KIND, int BI, int BJ, int NWI, int NWJ, bool PHASED>
-__global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel(const Product a) {
+constexpr int kWaves = 8, NWI = 2, NWJ = 4;   // wavefronts of a workgroup, along P and along Q
+constexpr int kBJ = 256;                      // rows per tile
+constexpr int kFlatStages = 3;
+// Tiles of 256 along P in two stages, or of 128 in three.
+constexpr int kLdsTiles = std::max(2 * (256 + kBJ) * kBK * 2, kFlatStages * (128 + kBJ) * kBK * 2);
+
+// Whether tiles of 128 along P take fewer rounds of the workgroups, a round of them being NARROW/WIDE as long.
+__device__ __forceinline__ bool narrow_tiles(int64_t blocks, int width, int workgroups) {
+    const int64_t wide = (blocks * ((width + 255) / 256) + workgroups - 1) / workgroups;
+    const int64_t narrow = (blocks * ((width + 127) / 128) + workgroups - 1) / workgroups;
+    return 5 * narrow < 8 * wide;
+}
+
+// All tiles of one workgroup, BI indices of P by kBJ of Q.
+template <int KIND, int BI>
+__device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table) {
+    constexpr int BJ = kBJ, NW = kWaves;
+    constexpr bool PHASED = BI == 256;
     constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
     constexpr int WI = BI / NWI, WJ = BJ / NWJ, IT = WI / 16, JT = WJ / 16;
-    constexpr int NW = NWI * NWJ;
     using P = Operand<BI, kPK, NW>;
     using Q = Operand<BJ, kQK, NW>;
     constexpr int kStage = P::kBytes + Q::kBytes;
     constexpr int kLoads = P::kLoads + Q::kLoads;
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    Table* table = (Table*)(lds + 2 * kStage);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave % NWI, wj = wave / NWI;
 
@@ -258,11 +271,6 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
     // times blocks along I.  A gated tile holds BI/2 outputs: their gate and their up columns.
     const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
     const int ni = (a.I + bi - 1) / bi;
-    if (wave == 0) {
-        const bool cut = scan_blocks(a.win, BJ, table, lane);
-        if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && lane == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
-    }
-    __syncthreads();
     const int weight_blocks = KIND == GRAD_WEIGHTS ? (a.J + BJ - 1) / BJ : 0;
     const int nj = KIND == GRAD_WEIGHTS ? a.win.L * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[a.win.L]);
     const int64_t tiles = (int64_t)nj * ni;
@@ -292,7 +300,7 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
     P p;
     Q q;
     auto steps_of = [&](const Tile& c) { return ((KIND == GRAD_WEIGHTS ? c.rows : a.Kc) + kBK - 1) / kBK; };
-    // Points the operands at a tile and issues its first loads: all of step 0, and of step 1 what its phase 0 reads.
+    // Points the operands at a tile and issues its first loads: all of step 0, and of step 1 all (or what its phase 0 reads).
     auto begin = [&](const Tile& c) {
         const int lane = opaque(threadIdx.x & 63);
         const uint16_t* pb = a.p + c.e * a.p_expert;
@@ -317,10 +325,20 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
             p.template load<0, P::kLoads>(lds, Kc, wave);
             q.template load<0, Q::kLoads>(lds + P::kBytes, Kc, wave);
             p.next(); q.next();
-            if (PHASED && Kc > kBK) {
-                p.template load<0, 1>(lds + kStage, Kc - kBK, wave);
-                p.template load<2, 3>(lds + kStage, Kc - kBK, wave);
-                q.template load<0, 4>(lds + kStage + P::kBytes, Kc - kBK, wave);
+            if constexpr (PHASED) {
+                if (Kc > kBK) {
+                    p.template load<0, 1>(lds + kStage, Kc - kBK, wave);
+                    p.template load<2, 3>(lds + kStage, Kc - kBK, wave);
+                    q.template load<0, 4>(lds + kStage + P::kBytes, Kc - kBK, wave);
+                }
+            } else {
+#pragma unroll
+                for (int k = 1; k < kFlatStages - 1; ++k) {
+                    if (k * kBK >= Kc) break;
+                    p.template load<0, P::kLoads>(lds + k * kStage, Kc - k * kBK, wave);
+                    q.template load<0, Q::kLoads>(lds + k * kStage + P::kBytes, Kc - k * kBK, wave);
+                    p.next(); q.next();
+                }
             }
         }
     };
@@ -432,18 +450,26 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
             }
             if (steps && !late) barrier();
         } else {
+            // Three stages, the loads of the step after next under way while one is multiplied, one barrier per step: it
+            // tells that everybody's part of the step's tile has landed, and that the place of the step before is free.
+            const bool idle = KIND != GRAD_WEIGHTS && wj * WJ >= c.rows - c.j0;   // none of the wavefront's rows exist
+            int stage = 0;
             for (int k = 0; k < steps; ++k) {
-                const char* cur = lds + (k & 1) * kStage;
-                if (k + 1 < steps) {
-                    char* nxt = lds + ((k + 1) & 1) * kStage;
-                    p.template load<0, P::kLoads>(nxt, Kc - (k + 1) * kBK, wave);
-                    q.template load<0, Q::kLoads>(nxt + P::kBytes, Kc - (k + 1) * kBK, wave);
-                    p.next(); q.next();
-                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-                } else {
-                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                }
+                const char* cur = lds + stage * kStage;
+                // besides the next step's loads the results stored since may be on their way at first: at least IT * JT / 2
+                // per lane (gated: half)
+                if (k + 1 >= steps) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                else if (k > 0 || fresh) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+                else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads + (KIND == FORWARD ? IT * JT / 4 : IT * JT / 2)) : "memory");
                 barrier();
+                if (k + 2 < steps) {
+                    char* to = lds + (stage == 0 ? 2 : stage - 1) * kStage;
+                    p.template load<0, P::kLoads>(to, Kc - (k + 2) * kBK, wave);
+                    q.template load<0, Q::kLoads>(to + P::kBytes, Kc - (k + 2) * kBK, wave);
+                    p.next(); q.next();
+                }
+                stage = stage == 2 ? 0 : stage + 1;
+                if (idle) continue;
                 bf16x8 pf[2][IT], qf[2][JT];
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
@@ -467,10 +493,9 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
                         for (int jt = 0; jt < JT; ++jt)
                             sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jt], sums[jt], 0, 0, 0);
                 }
-                // every wavefront has read the tile before anybody loads into its place
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                barrier();
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before the barrier of the next step says so
             }
+            if (steps) barrier();
         }
 
         // The next tile's first loads run while this one's results are written.
@@ -609,6 +634,20 @@ __global__ __launch_bounds__(64 * NWI * NWJ, PHASED ? 2 : 1) void product_kernel
     }
 }
 
+template <int KIND>
+__global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    Table* table = (Table*)(lds + kLdsTiles);
+    if (threadIdx.x < 64) {
+        const bool cut = scan_blocks(a.win, kBJ, table, threadIdx.x);
+        if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
+    }
+    __syncthreads();
+    const int64_t blocks = KIND == GRAD_WEIGHTS ? (int64_t)a.win.L * ((a.J + kBJ - 1) / kBJ) : __builtin_amdgcn_readfirstlane(table->starts[a.win.L]);
+    if (narrow_tiles(blocks, a.I * (KIND == FORWARD && a.gated ? 2 : 1), gridDim.x)) product_tiles<KIND, 128>(a, lds, table);
+    else product_tiles<KIND, 256>(a, lds, table);
+}
+
 // grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows.
 constexpr int kActRows = 16;
 
@@ -662,15 +701,15 @@ int64_t most_blocks(const Windows& w, int rows) {
 }
 
 template <int KIND>
-hipError_t launch(const Product& a, int64_t most_rows_blocks, hipStream_t s) {
-    constexpr int BI = 256, BJ = 256, NWI = 2, NWJ = 4;
-    constexpr int lds = 2 * (BI + BJ) * kBK * 2 + (int)sizeof(Table);
-    const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
-    const int64_t most = most_rows_blocks * ((a.I + bi - 1) / bi);
+hipError_t launch(const Product& a, int64_t most_row_blocks, hipStream_t s) {
+    constexpr int lds = kLdsTiles + (int)sizeof(Table);
+    static_assert(lds <= 160 * 1024, "a compute unit's LDS");
+    const int bi = KIND == FORWARD && a.gated ? 64 : 128;   // of the narrow tiles
+    const int64_t most = most_row_blocks * ((a.I + bi - 1) / bi);
     if (most <= 0) return hipSuccess;
     const int64_t cus = std::max(8, compute_units() / 8 * 8);
     const int64_t grid = std::min(cus, (most + 7) / 8 * 8);
-    hipLaunchKernelGGL((product_kernel<KIND, BI, BJ, NWI, NWJ, true>), dim3((uint32_t)grid), dim3(64 * NWI * NWJ), lds, s, a);
+    hipLaunchKernelGGL(product_kernel<KIND>, dim3((uint32_t)grid), dim3(64 * kWaves), lds, s, a);
     return hipGetLastError();
 }
 
@@ -698,7 +737,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     p.pre = a.pre.base; p.pre_expert = a.pre.expert_stride; p.pre_row = a.pre.row_stride;
     p.res = a.res.base; p.res_expert = a.res.expert_stride; p.res_row = a.res.row_stride;
     p.status = a.status;
-    return launch<FORWARD>(p, most_blocks(a.win, 256), s);
+    return launch<FORWARD>(p, most_blocks(a.win, kBJ), s);
 }
 
 hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
@@ -708,7 +747,7 @@ hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
     p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
     p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
     p.I = a.Kd; p.Kc = a.N;
-    return launch<GRAD_ROWS>(p, most_blocks(a.win, 256), s);
+    return launch<GRAD_ROWS>(p, most_blocks(a.win, kBJ), s);
 }
 
 hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
@@ -720,7 +759,7 @@ hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
     p.out_f32 = a.gw_f32; p.accumulate = a.accumulate;
     p.grad_b = a.grad_b; p.gb_stride = a.gb_stride;
     p.I = a.Kd; p.J = a.N;
-    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + 255) / 256), s);
+    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + kBJ - 1) / kBJ), s);
 }
 
 hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s) {
