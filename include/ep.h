@@ -710,7 +710,8 @@ EP_API ep_result_t ep_expert_layer_plan(int64_t num_tokens, int32_t top_k, int32
  *     out[t] = r[t] + sum over k with a local expert of w[t,k] * (W2_e act(W1_e x[t] + b1_e) + b2_e)
  * e = idx[t,k] - first_expert; ids outside [first_expert, first_expert + L) (-1, other ranks' experts)
  * contribute nothing.  An expert may be named twice by a token.  w * act(.) is rounded to bf16 between the
- * two products; sums are float32 in a fixed order.  H and I multiples of 8, at most 2^17.
+ * two products; sums are float32 in a fixed order.  H and I multiples of 8, at most 2^17; rows on
+ * 16-byte boundaries, less than 2^22 elements apart.
  * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED (more than 128 tokens), EP_ERR_HIP.
  */
 EP_API ep_result_t ep_expert_layer(const ep_product_config_t *cfg, const ep_tensor_t *inputs, int32_t num_inputs,

@@ -131,8 +131,9 @@ struct LayerArgs {
 
 // Where the parts of the layer's workspace lie (bytes from its start).
 struct LayerPlan {
-    int64_t mid, members, total;
+    int64_t mid, total;          // the sorted entries come first, then the rows between the products
     int slots;                   // experts that can be named: min(L, T * K)
+    int up_parts;                // workgroups per named expert in the first launch
 };
 void plan_layer(int T, int K, int L, int H, int inner, LayerPlan* p);
 hipError_t launch_layer(const LayerArgs& a, hipStream_t s);

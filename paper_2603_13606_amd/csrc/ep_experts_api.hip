@@ -295,7 +295,7 @@ ep_result_t ep_expert_layer(const ep_product_config_t* cfg, const ep_tensor_t* i
     if (T < 0 || K < 1 || K > kMaxTopK || I % 8 || H > kMaxLayerExtent || I > kMaxLayerExtent) return EP_ERR_INVALID_ARG;
     if (down->shape[0] != L || down->shape[1] != H || down->shape[2] != I) return EP_ERR_INVALID_ARG;
     auto token_rows = [&](const ep_tensor_t* t) {
-        return check_2d(t, EP_DTYPE_BF16, T, H, true) && t->stride[0] % 8 == 0 && aligned16(t->data);
+        return check_2d(t, EP_DTYPE_BF16, T, H, true) && t->stride[0] % 8 == 0 && t->stride[0] < kMaxExtent && aligned16(t->data);
     };
     if (!token_rows(x) || !token_rows(out) || (res && !token_rows(res))) return EP_ERR_INVALID_ARG;
     if (!check_2d(idx, EP_DTYPE_I32, T, K, true) || (w && !check_2d(w, EP_DTYPE_F32, T, K, true))) return EP_ERR_INVALID_ARG;

@@ -3,14 +3,15 @@
 //   out[t] = res[t] + sum_k w[t,k] (W2_e act(W1_e x[t] + b1_e) + b2_e),  e = topk_idx[t,k], local experts only
 //
 // What bounds it is reading the weights of the experts that are named, once.  Both kernels therefore stream
-// weight rows from memory into registers as the left operand of MFMA 16x16x32, 16 rows at a time, the tokens
-// that name the expert (up to 16 per instruction) being the right operand:
-//   up    a workgroup per (named expert, 16 rows of the inner dimension): the contraction over H is split over
-//         its wavefronts and joined through LDS in wave order; bias, activation and gate weight are applied in
-//         float32, and one row per (token, expert) goes to the workspace in bf16.
+// weight rows from memory into registers as the left operand of MFMA 16x16x32, 16 rows at a time and several
+// blocks ahead, the tokens that name the expert (up to 16 per instruction) being the right operand:
+//   up    a workgroup per (named expert, some runs of 16 rows of the inner dimension): the contraction over H is split
+//         over its wavefronts and joined through LDS in wave order; bias, activation and gate weight are applied in
+//         float32, and one row per (token, expert) goes to the workspace in bf16.  One more workgroup sorts the
+//         routed entries by expert for the second launch.
 //   down  a workgroup per 16 columns of the output: its wavefronts share out the (expert, part of the inner
 //         dimension) pairs evenly, each adds up its own part of the output for all tokens in LDS, and the
-//         parts are joined in wave order.  No atomics: results do not depend on timing.
+//         parts are joined in wave order.  No atomics on values: results do not depend on timing.
 // An expert works on its own tokens only, so what its weights hold (an infinity, a NaN) reaches no others.
 #include <algorithm>
 
@@ -23,14 +24,25 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kUpWaves = 4, kDownWaves = 8;
-constexpr int kRows = 16;     // weight rows per workgroup
+constexpr int kUpDepth = 4, kDownDepth = 4;   // blocks of weights on their way per wavefront
+constexpr int kRows = 16;     // weight rows per run
 constexpr int kBlock = 64;    // contraction indices per step of a wavefront: whole 128-byte lines of 16 rows
+constexpr int kGroups = 4;    // groups of 16 tokens per pass over the weights
+constexpr uint32_t kNowhere = 0x80000000u;  // offset of a lane that has nothing to load: reads zeros
 
-// members of slot s: {expert, n, then n pairs {token, row of the workspace}}; one slot per named expert
-__host__ __device__ constexpr int member_words(int T) { return 2 + 2 * T; }
+// The routed entries by expert, as the second launch wants them (in the workspace): the number of named experts, their
+// ids and where their entries start (one more than there are experts), then the entries, token << 16 | row of the
+// workspace.  A token that names an expert twice has one entry.
+struct Sorted {
+    int32_t *count, *expert, *start, *entry;
+};
+__host__ __device__ constexpr int64_t sorted_words(int slots, int entries) { return 1 + slots + slots + 1 + entries; }
+__host__ __device__ inline Sorted sorted_at(uint8_t* base, int slots) {
+    int32_t* p = (int32_t*)base;
+    return {p, p + 1, p + 1 + slots, p + 2 + 2 * slots};
+}
 
 __device__ __forceinline__ float load_bias(const void* b, int64_t i, int is_f32) {
     return is_f32 ? ((const float*)b)[i] : bf16_f32(((const uint16_t*)b)[i]);
@@ -42,56 +54,161 @@ __device__ __forceinline__ int local_id(const LayerArgs& a, int t, int k) {
     return e >= 0 && e < a.L ? (int)e : -1;
 }
 
-__device__ __forceinline__ bf16x8 load8(const uint16_t* p, bool there) {
-    u32x4 v = {0, 0, 0, 0};
-    if (there) v = *(const u32x4*)p;
-    return __builtin_bit_cast(bf16x8, v);
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00027000);
 }
 
-// acc[g][jt] += 16 weight rows (of each of G matrices) x the tokens of JT groups of 16, over the blocks
-// [b0, b1) with the given stride of the contraction.
-template <int G, int JT>
-__device__ __forceinline__ void multiply(f32x4 (&acc)[G][8], const uint16_t* const (&w)[G], const uint16_t* const (&x)[8],
-                                         const bool (&there)[8], int b0, int b1, int stride, int K, int lane) {
-    for (int b = b0; b < b1; b += stride) {
-        bf16x8 wf[G][2], xf[JT][2];
+__device__ __forceinline__ bf16x8 load8(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+}
+
+// The weights of a block (16 rows of 128 bytes per matrix) go to LDS without passing through registers: the eight lanes of
+// a row load a whole line in one instruction, which is what lets the non-temporal hint pay (a plain sweep over rows, TB/s:
+// whole lines with the hint 7.0 to 7.3, without 6.2 to 6.5; half lines, as the matrix instruction wants its operand, 6.2
+// without and 5.5 to 6.0 with it).  The unit u of row r lies at u ^ (r & 7): a fragment read touches all banks.  Each
+// wavefront has a ring of its own, no barriers.
+constexpr int kWeightBlock = kRows * kBlock * 2;
+constexpr int kNonTemporal = 2;   // cache policy bit of a buffer load
+
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+// acc[g][jt] += 16 weight rows (of each of G matrices) x the tokens of JT groups of 16, over the blocks b0, b0 + stride, ..
+// below b1 of the contraction (K indices in all), DEPTH of them on their way at any time.  wo: the lane's offset in the first
+// and in the second eight weight rows, its unit included; xo: its token's row in each group, kNowhere if there is none.
+template <int G, int JT, int DEPTH>
+__device__ __forceinline__ void multiply(f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
+                                         __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride, int K,
+                                         int lane) {
+    constexpr int kLoads = 2 * (G + JT);   // per block
+    bf16x8 xf[DEPTH][JT][2];
+    const int wk = ((lane & 7) ^ (lane >> 3)) * 8, xk = (lane >> 4) * 8;
+    auto load = [&](int d, int b) {
+        const bool in = b < b1 && b * kBlock + wk < K;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(w[g], (lds_ptr)(ring + (d * G + g) * kWeightBlock + s * 1024), 16,
+                                                         in ? wo[s] + b * (kBlock * 2) : kNowhere, 0, 0, kNonTemporal);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int k = b * kBlock + s * 32 + (lane >> 4) * 8;
-            const bool in = k < K;
+            const int k = b * kBlock + s * 32 + xk;
 #pragma unroll
-            for (int g = 0; g < G; ++g) wf[g][s] = load8(w[g] + k, in);
-#pragma unroll
-            for (int jt = 0; jt < JT; ++jt) xf[jt][s] = load8(x[jt] + k, in && there[jt]);
+            for (int jt = 0; jt < JT; ++jt) xf[d][jt][s] = load8(x, b < b1 && k < K ? xo[jt] + k * 2 : kNowhere);
         }
+    };
+    const char* mine = ring + (lane & 15) * 128;
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+    for (int d = 0; d < DEPTH; ++d) load(d, b0 + d * stride);
+    for (int b = b0; b < b1; b += DEPTH * stride) {
 #pragma unroll
-            for (int g = 0; g < G; ++g)
+        for (int d = 0; d < DEPTH; ++d) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * kLoads) : "memory");
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int jt = 0; jt < JT; ++jt)
-                    acc[g][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[g][s], xf[jt][s], acc[g][jt], 0, 0, 0);
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const bf16x8 wf = *(const bf16x8*)(mine + (d * G + g) * kWeightBlock + (((s * 4 + (lane >> 4)) ^ (lane & 7)) << 4));
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt)
+                        acc[g][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[d][jt][s], acc[g][jt], 0, 0, 0);
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the block has been read before its place is loaded again
+            __builtin_amdgcn_sched_barrier(0);
+            load(d, b + (DEPTH + d) * stride);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing writes to the ring any more
+}
+
+// By the number of tokens: the more groups, the fewer blocks of them fit the registers.
+template <int G, int DEPTH>
+__device__ __forceinline__ void multiply_groups(int n, f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
+                                                __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride,
+                                                int K, int lane) {
+    if (n <= 16) multiply<G, 1, DEPTH>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
+    else if (n <= 32) multiply<G, 2, 3>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
+    else multiply<G, 4, 2>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
+}
+
+// The lane's offsets in the two halves of 16 weight rows `stride` elements apart, of which `rows` exist.
+__device__ __forceinline__ void weight_offsets(uint32_t (&wo)[2], int64_t stride, int rows, int lane) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int r = s * 8 + (lane >> 3);
+        wo[s] = r < rows ? (uint32_t)(r * stride * 2) + (((lane & 7) ^ (lane >> 3)) << 4) : kNowhere;
+    }
+}
+
+// The routed entries sorted by expert, by one workgroup.  The order of an expert's entries is arbitrary: each token's
+// column is a sum of its own.
+__device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan& plan, int* fill) {
+    const Sorted out = sorted_at(a.workspace, plan.slots);
+    for (int e = threadIdx.x; e < kMaxExperts; e += 64 * kUpWaves) fill[e] = 0;
+    __syncthreads();
+    auto entry_id = [&](int i) {
+        const int t = i / a.K, k = i - t * a.K, e = local_id(a, t, k);
+        for (int q = 0; q < k && e >= 0; ++q)
+            if (local_id(a, t, q) == e) return -1;
+        return e;
+    };
+    for (int i = threadIdx.x; i < a.T * a.K; i += 64 * kUpWaves) {
+        const int e = entry_id(i);
+        if (e >= 0) atomicAdd(&fill[e], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        constexpr int kPer = kMaxExperts / 64;
+        const int lane = threadIdx.x, e0 = lane * kPer;
+        int sum = 0, named = 0;
+        for (int e = e0; e < e0 + kPer; ++e) {
+            sum += fill[e];
+            named += fill[e] > 0;
+        }
+        int s1 = sum, n1 = named;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int v = __shfl_up(s1, d), u = __shfl_up(n1, d);
+            if (lane >= d) { s1 += v; n1 += u; }
+        }
+        int at = s1 - sum, slot = n1 - named;
+        for (int e = e0; e < e0 + kPer; ++e) {
+            const int n = fill[e];
+            fill[e] = at;
+            if (n > 0) {
+                out.expert[slot] = e;
+                out.start[slot] = at;
+                ++slot;
+                at += n;
+            }
+        }
+        if (lane == 63) {
+            *out.count = n1;
+            out.start[n1] = s1;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.T * a.K; i += 64 * kUpWaves) {
+        const int e = entry_id(i);
+        if (e >= 0) out.entry[atomicAdd(&fill[e], 1)] = (i / a.K) << 16 | i;
     }
 }
 
 template <int G>
-__device__ __forceinline__ void multiply_groups(int n, f32x4 (&acc)[G][8], const uint16_t* const (&w)[G], const uint16_t* const (&x)[8],
-                                                const bool (&there)[8], int b0, int b1, int stride, int K, int lane) {
-    if (n <= 16) multiply<G, 1>(acc, w, x, there, b0, b1, stride, K, lane);
-    else if (n <= 32) multiply<G, 2>(acc, w, x, there, b0, b1, stride, K, lane);
-    else if (n <= 64) multiply<G, 4>(acc, w, x, there, b0, b1, stride, K, lane);
-    else multiply<G, 8>(acc, w, x, there, b0, b1, stride, K, lane);
-}
-
-template <int G>
-__global__ __launch_bounds__(64 * kUpWaves) void layer_up_kernel(const LayerArgs a, const LayerPlan plan, int slices) {
+__global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerArgs a, const LayerPlan plan) {
+    // each wavefront's ring of weights; afterwards its part of the sums, or the sort's counters
+    __shared__ __attribute__((aligned(1024))) char rings[kUpWaves][kUpDepth * G * kWeightBlock];
     __shared__ uint32_t named[kMaxExperts / 32];
     __shared__ int s_n[2];
     __shared__ int s_token[kLayerMaxTokens], s_row[kLayerMaxTokens];
     __shared__ float s_gate[kLayerMaxTokens];
-    __shared__ float part[kUpWaves][G][16 * 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int slot = blockIdx.x / slices, slice = blockIdx.x % slices;
+    if (blockIdx.x == 0) {
+        sort_entries(a, plan, (int*)rings);
+        return;
+    }
+    const int slot = (blockIdx.x - 1) / plan.up_parts, part = (blockIdx.x - 1) % plan.up_parts;
 
     // the slot-th of the experts that any token names
     if (threadIdx.x < kMaxExperts / 32) named[threadIdx.x] = 0;
@@ -108,12 +225,8 @@ __global__ __launch_bounds__(64 * kUpWaves) void layer_up_kernel(const LayerArgs
         const int v = __shfl_up(upto, d);
         if (lane >= d) upto += v;
     }
-    int* members = (int*)(a.workspace + plan.members);
-    const int total = __shfl(upto, 63);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *(int*)a.workspace = total;
-    if (slot >= total) return;
-    const uint64_t before = __ballot(upto <= slot);
-    const int at = __builtin_popcountll(before);  // the word that holds it: the counts only grow
+    if (slot >= __shfl(upto, 63)) return;
+    const int at = __builtin_popcountll(__ballot(upto <= slot));  // the word that holds it: the counts only grow
     uint32_t bits = (uint32_t)__builtin_amdgcn_readlane((int)word, at);
     for (int skip = slot - (__shfl(upto, at) - __popc(bits)); skip > 0; --skip) bits &= bits - 1;
     const int e = __builtin_amdgcn_readfirstlane(at * 32 + __builtin_ctz(bits));
@@ -142,99 +255,102 @@ __global__ __launch_bounds__(64 * kUpWaves) void layer_up_kernel(const LayerArgs
         s_gate[pos] = gate;
     }
     __syncthreads();
-    if (slice == 0) {
-        int* m = members + slot * member_words(a.T);
-        if (threadIdx.x == 0) { m[0] = e; m[1] = n; }
-        if ((int)threadIdx.x < n) { m[2 + 2 * threadIdx.x] = s_token[threadIdx.x]; m[3 + 2 * threadIdx.x] = s_row[threadIdx.x]; }
-    }
 
-    const int i0 = slice * kRows;
-    const int i = min(i0 + (lane & 15), a.inner - 1);
-    const uint16_t* w[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) w[g] = a.w_up + e * a.up_expert + (int64_t)(i + g * a.inner) * a.up_row;
-    const uint16_t* x[8];
-    bool there[8];
-#pragma unroll
-    for (int jt = 0; jt < 8; ++jt) {
-        const int pos = jt * 16 + (lane & 15);
-        there[jt] = pos < n;
-        x[jt] = a.x + (there[jt] ? s_token[pos] : 0) * a.x_stride;
-    }
-    f32x4 acc[G][8];
-#pragma unroll
-    for (int g = 0; g < G; ++g)
-#pragma unroll
-        for (int jt = 0; jt < 8; ++jt) acc[g][jt] = f32x4{0, 0, 0, 0};
-    multiply_groups<G>(n, acc, w, x, there, wave, (a.H + kBlock - 1) / kBlock, kUpWaves, a.H, lane);
-
+    const auto x = buffer(a.x);
     uint16_t* mid = (uint16_t*)(a.workspace + plan.mid);
+    const int blocks = (a.H + kBlock - 1) / kBlock;
+    const int slices = (a.inner + kRows - 1) / kRows;
+    for (int slice = part; slice < slices; slice += plan.up_parts) {
+        const int i0 = slice * kRows;
+        uint32_t wo[2];
+        weight_offsets(wo, a.up_row, a.inner - i0, lane);
+        __amdgpu_buffer_rsrc_t w[G];
 #pragma unroll
-    for (int jt = 0; jt < 8; ++jt) {
-        if (jt * 16 >= n) break;
+        for (int g = 0; g < G; ++g) w[g] = buffer(a.w_up + e * a.up_expert + (int64_t)(i0 + g * a.inner) * a.up_row);
+        for (int p0 = 0; p0 < n; p0 += kGroups * 16) {
+            uint32_t xo[kGroups];
+            f32x4 acc[G][kGroups];
 #pragma unroll
-        for (int g = 0; g < G; ++g)
-            *(f32x4*)&part[wave][g][(lane & 15) * 16 + (lane >> 4) * 4] = acc[g][jt];
-        __syncthreads();
-        const int pos = jt * 16 + (threadIdx.x >> 4), ii = i0 + (threadIdx.x & 15);
-        if (pos < n && ii < a.inner) {
-            float v[G];
+            for (int jt = 0; jt < kGroups; ++jt) {
+                const int pos = p0 + jt * 16 + (lane & 15);
+                xo[jt] = pos < n ? (uint32_t)(s_token[pos] * a.x_stride * 2) : kNowhere;
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                v[g] = a.b_up ? load_bias(a.b_up, e * a.b_up_stride + ii + g * a.inner, a.b_up_f32) : 0.0f;
-#pragma unroll
-                for (int q = 0; q < kUpWaves; ++q) v[g] += part[q][g][threadIdx.x];
+                for (int g = 0; g < G; ++g) acc[g][jt] = f32x4{0, 0, 0, 0};
             }
-            float h = activate(a.act, v[0]);
-            if (G == 2) h *= v[G - 1];
-            // the gate weight goes in before the rounding to bf16: one rounding of the product of both
-            mid[(int64_t)s_row[pos] * a.inner + ii] = (uint16_t)pack2_bf16(h * s_gate[pos], 0.0f);
+            multiply_groups<G, kUpDepth>(n - p0, acc, w, wo, x, xo, rings[wave], wave, blocks, kUpWaves, a.H, lane);
+#pragma unroll
+            for (int jt = 0; jt < kGroups; ++jt) {
+                if (p0 + jt * 16 >= n) break;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    *(f32x4*)((float*)rings[wave] + g * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[g][jt];
+                __syncthreads();
+                const int pos = p0 + jt * 16 + (threadIdx.x >> 4), ii = i0 + (threadIdx.x & 15);
+                if (pos < n && ii < a.inner) {
+                    float v[G];
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        v[g] = a.b_up ? load_bias(a.b_up, e * a.b_up_stride + ii + g * a.inner, a.b_up_f32) : 0.0f;
+#pragma unroll
+                        for (int q = 0; q < kUpWaves; ++q) v[g] += ((const float*)rings[q])[g * 256 + threadIdx.x];
+                    }
+                    float h = activate(a.act, v[0]);
+                    if (G == 2) h *= v[G - 1];
+                    // the gate weight goes in before the rounding to bf16: one rounding of the product of both
+                    mid[(int64_t)s_row[pos] * a.inner + ii] = (uint16_t)pack2_bf16(h * s_gate[pos], 0.0f);
+                }
+                __syncthreads();
+            }
         }
-        __syncthreads();
     }
 }
 
-__global__ __launch_bounds__(64 * kDownWaves) void layer_down_kernel(const LayerArgs a, const LayerPlan plan) {
-    extern __shared__ __attribute__((aligned(16))) float sums[];  // [waves][T][16]
+__global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const LayerArgs a, const LayerPlan plan) {
+    // each wavefront's ring of weights, its part of the output [T][16], then the sorted entries
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    float* sums = (float*)(lds + kDownWaves * kDownDepth * kWeightBlock);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h0 = blockIdx.x * kRows;
-    const int total = __builtin_amdgcn_readfirstlane(*(const int*)a.workspace);
-    const int* members = (const int*)(a.workspace + plan.members);
-    const uint16_t* mid = (const uint16_t*)(a.workspace + plan.mid);
+    int32_t* words = (int32_t*)(sums + kDownWaves * a.T * 16);
+    for (int i = threadIdx.x; i < (int)sorted_words(plan.slots, a.T * a.K); i += 64 * kDownWaves) words[i] = ((const int32_t*)a.workspace)[i];
+    for (int i = threadIdx.x; i < kDownWaves * a.T * 16; i += 64 * kDownWaves) sums[i] = 0.0f;
+    __syncthreads();
+    const Sorted table = sorted_at((uint8_t*)words, plan.slots);
     float* mine = sums + wave * a.T * 16;
-    for (int i = lane; i < a.T * 16; i += 64) mine[i] = 0.0f;
 
+    const auto x = buffer(a.workspace + plan.mid);
     const int blocks = (a.inner + kBlock - 1) / kBlock;
-    const int64_t items = (int64_t)total * blocks;
+    const int64_t items = (int64_t)*table.count * blocks;
     int64_t q = items * wave / kDownWaves;
     const int64_t end = items * (wave + 1) / kDownWaves;
-    const int h = min(h0 + (lane & 15), a.H - 1);
+    char* ring = lds + wave * (kDownDepth * kWeightBlock);
+    uint32_t wo[2];
+    weight_offsets(wo, a.down_row, a.H - h0, lane);
     while (q < end) {
         const int slot = (int)(q / blocks), b0 = (int)(q - (int64_t)slot * blocks);
         const int b1 = (int)min((int64_t)blocks, b0 + (end - q));
-        const int* m = members + slot * member_words(a.T);
-        const int e = __builtin_amdgcn_readfirstlane(m[0]), n = __builtin_amdgcn_readfirstlane(m[1]);
-        const uint16_t* w[1] = {a.w_down + e * a.down_expert + (int64_t)h * a.down_row};
-        const uint16_t* x[8];
-        bool there[8];
-        int token[8];
+        const int e = __builtin_amdgcn_readfirstlane(table.expert[slot]), first = __builtin_amdgcn_readfirstlane(table.start[slot]);
+        const int n = __builtin_amdgcn_readfirstlane(table.start[slot + 1]) - first;
+        const __amdgpu_buffer_rsrc_t w[1] = {buffer(a.w_down + e * a.down_expert + (int64_t)h0 * a.down_row)};
+        for (int p0 = 0; p0 < n; p0 += kGroups * 16) {
+            uint32_t xo[kGroups];
+            f32x4 acc[1][kGroups];
 #pragma unroll
-        for (int jt = 0; jt < 8; ++jt) {
-            const int pos = jt * 16 + (lane & 15);
-            there[jt] = pos < n;
-            token[jt] = there[jt] ? m[2 + 2 * pos] : 0;
-            x[jt] = mid + (int64_t)(there[jt] ? m[3 + 2 * pos] : 0) * a.inner;
-        }
-        f32x4 acc[1][8];
-#pragma unroll
-        for (int jt = 0; jt < 8; ++jt) acc[0][jt] = f32x4{0, 0, 0, 0};
-        multiply_groups<1>(n, acc, w, x, there, b0, b1, 1, a.inner, lane);
-#pragma unroll
-        for (int jt = 0; jt < 8; ++jt)
-            if (there[jt]) {
-                f32x4* to = (f32x4*)(mine + token[jt] * 16 + (lane >> 4) * 4);
-                *to = *to + acc[0][jt];
+            for (int jt = 0; jt < kGroups; ++jt) {
+                const int pos = p0 + jt * 16 + (lane & 15);
+                xo[jt] = pos < n ? (uint32_t)(table.entry[first + pos] & 0xffff) * (uint32_t)a.inner * 2 : kNowhere;
+                acc[0][jt] = f32x4{0, 0, 0, 0};
             }
+            multiply_groups<1, kDownDepth>(n - p0, acc, w, wo, x, xo, ring, b0, b1, 1, a.inner, lane);
+#pragma unroll
+            for (int jt = 0; jt < kGroups; ++jt) {
+                const int pos = p0 + jt * 16 + (lane & 15);
+                if (pos < n) {
+                    f32x4* to = (f32x4*)(mine + (table.entry[first + pos] >> 16) * 16 + (lane >> 4) * 4);
+                    *to = *to + acc[0][jt];
+                }
+            }
+        }
         q += b1 - b0;
     }
     __syncthreads();
@@ -255,25 +371,32 @@ __global__ __launch_bounds__(64 * kDownWaves) void layer_down_kernel(const Layer
 
 int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
+int64_t down_lds(int T, int K, int slots) {
+    return kDownWaves * (kDownDepth * kWeightBlock + (int64_t)T * 16 * 4) + sorted_words(slots, T * K) * 4;
+}
+
 }  // namespace
 
 void plan_layer(int T, int K, int L, int H, int inner, LayerPlan* p) {
     p->slots = (int)std::min<int64_t>(L, (int64_t)T * K);
-    p->members = 256;  // the number of named experts comes first
-    p->mid = p->members + up256((int64_t)p->slots * member_words(T) * 4);
+    p->mid = up256(sorted_words(p->slots, T * K) * 4);
     p->total = p->mid + up256((int64_t)T * K * inner * 2);
+    p->up_parts = 0;
 }
 
 hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
     if (a.T == 0) return hipSuccess;
     LayerPlan plan;
     plan_layer(a.T, a.K, a.L, a.H, a.inner, &plan);
+    const int cus = compute_units();
+    // up: two workgroups share a compute unit; beyond four for each a workgroup takes several runs of rows, which spares
+    // the search for its expert's tokens
     const int slices = (a.inner + kRows - 1) / kRows;
-    const dim3 grid((uint32_t)(plan.slots * slices));
-    if (a.gated) hipLaunchKernelGGL(layer_up_kernel<2>, grid, dim3(64 * kUpWaves), 0, s, a, plan, slices);
-    else hipLaunchKernelGGL(layer_up_kernel<1>, grid, dim3(64 * kUpWaves), 0, s, a, plan, slices);
-    const size_t lds = (size_t)kDownWaves * a.T * 16 * sizeof(float);
-    hipLaunchKernelGGL(layer_down_kernel, dim3((uint32_t)((a.H + kRows - 1) / kRows)), dim3(64 * kDownWaves), lds, s, a, plan);
+    plan.up_parts = std::clamp((4 * cus + plan.slots - 1) / plan.slots, 1, slices);
+    const dim3 grid((uint32_t)(plan.slots * plan.up_parts + 1));
+    if (a.gated) hipLaunchKernelGGL(layer_up_kernel<2>, grid, dim3(64 * kUpWaves), 0, s, a, plan);
+    else hipLaunchKernelGGL(layer_up_kernel<1>, grid, dim3(64 * kUpWaves), 0, s, a, plan);
+    hipLaunchKernelGGL(layer_down_kernel, dim3((uint32_t)((a.H + kRows - 1) / kRows)), dim3(64 * kDownWaves), down_lds(a.T, a.K, plan.slots), s, a, plan);
     return hipGetLastError();
 }
 
