@@ -68,33 +68,34 @@ __device__ __forceinline__ bf16x8 load8(__amdgpu_buffer_rsrc_t r, uint32_t off) 
 // without and 5.5 to 6.0 with it).  The unit u of row r lies at u ^ (r & 7): a fragment read touches all banks.  Each
 // wavefront has a ring of its own, no barriers.
 constexpr int kWeightBlock = kRows * kBlock * 2;
-constexpr int kNonTemporal = 2;   // cache policy bit of a buffer load
+constexpr int kNonTemporal = 2;   // cache policy bit of a buffer load: for weights whose rows start on lines
 
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 // acc[g][jt] += 16 weight rows (of each of G matrices) x the tokens of JT groups of 16, over the blocks b0, b0 + stride, ..
 // below b1 of the contraction (K indices in all), DEPTH of them on their way at any time.  wo: the lane's offset in the first
 // and in the second eight weight rows, its unit included; xo: its token's row in each group, kNowhere if there is none.
-template <int G, int JT, int DEPTH>
+template <int G, int JT, int DEPTH, int ROWS, bool NT>
 __device__ __forceinline__ void multiply(f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
                                          __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride, int K,
                                          int lane) {
-    constexpr int kLoads = 2 * (G + JT);   // per block
+    constexpr int kHalves = ROWS / 8, kLoads = kHalves * G + 2 * JT;   // per block
     bf16x8 xf[DEPTH][JT][2];
     const int wk = ((lane & 7) ^ (lane >> 3)) * 8, xk = (lane >> 4) * 8;
     auto load = [&](int d, int b) {
-        const bool in = b < b1 && b * kBlock + wk < K;
+        const int left = b < b1 ? K - b * kBlock : 0;
+        const uint32_t out = wk < left ? 0 : kNowhere;   // an offset with this bit is beyond the buffer's end
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < kHalves; ++s)
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(w[g], (lds_ptr)(ring + (d * G + g) * kWeightBlock + s * 1024), 16,
-                                                         in ? wo[s] + b * (kBlock * 2) : kNowhere, 0, 0, kNonTemporal);
+                                                         (wo[s] + b * (kBlock * 2)) | out, 0, 0, NT ? kNonTemporal : 0);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int k = b * kBlock + s * 32 + xk;
+            const uint32_t gone = s * 32 + xk < left ? 0 : kNowhere;
 #pragma unroll
-            for (int jt = 0; jt < JT; ++jt) xf[d][jt][s] = load8(x, b < b1 && k < K ? xo[jt] + k * 2 : kNowhere);
+            for (int jt = 0; jt < JT; ++jt) xf[d][jt][s] = load8(x, (xo[jt] + (b * kBlock + s * 32 + xk) * 2) | gone);
         }
     };
     const char* mine = ring + (lane & 15) * 128;
@@ -123,13 +124,13 @@ __device__ __forceinline__ void multiply(f32x4 (&acc)[G][kGroups], const __amdgp
 }
 
 // By the number of tokens: the more groups, the fewer blocks of them fit the registers.
-template <int G, int DEPTH>
+template <int G, int DEPTH, int ROWS, bool NT>
 __device__ __forceinline__ void multiply_groups(int n, f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
                                                 __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride,
                                                 int K, int lane) {
-    if (n <= 16) multiply<G, 1, DEPTH>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
-    else if (n <= 32) multiply<G, 2, 3>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
-    else multiply<G, 4, 2>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
+    if (n <= 16) multiply<G, 1, DEPTH, ROWS, NT>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
+    else if (n <= 32) multiply<G, 2, 3, ROWS, NT>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
+    else multiply<G, 4, 2, ROWS, NT>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
 }
 
 // The lane's offsets in the two halves of 16 weight rows `stride` elements apart, of which `rows` exist.
@@ -195,7 +196,8 @@ __device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan
     }
 }
 
-template <int G>
+// SPLIT: wavefronts that share the contraction of a run of rows, 4 or 1.
+template <int G, int SPLIT, bool NT>
 __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerArgs a, const LayerPlan plan) {
     // each wavefront's ring of weights; afterwards its part of the sums, or the sort's counters
     __shared__ __attribute__((aligned(1024))) char rings[kUpWaves][kUpDepth * G * kWeightBlock];
@@ -260,7 +262,9 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
     uint16_t* mid = (uint16_t*)(a.workspace + plan.mid);
     const int blocks = (a.H + kBlock - 1) / kBlock;
     const int slices = (a.inner + kRows - 1) / kRows;
-    for (int slice = part; slice < slices; slice += plan.up_parts) {
+    constexpr int kRuns = kUpWaves / SPLIT;   // of rows, next to each other
+    for (int slice = part * kRuns + wave / SPLIT; slice - wave / SPLIT < slices; slice += plan.up_parts * kRuns) {
+        if (SPLIT == 1 && slice >= slices) break;
         const int i0 = slice * kRows;
         uint32_t wo[2];
         weight_offsets(wo, a.up_row, a.inner - i0, lane);
@@ -277,40 +281,64 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
 #pragma unroll
                 for (int g = 0; g < G; ++g) acc[g][jt] = f32x4{0, 0, 0, 0};
             }
-            multiply_groups<G, kUpDepth>(n - p0, acc, w, wo, x, xo, rings[wave], wave, blocks, kUpWaves, a.H, lane);
-#pragma unroll
-            for (int jt = 0; jt < kGroups; ++jt) {
-                if (p0 + jt * 16 >= n) break;
+            multiply_groups<G, kUpDepth, kRows, NT>(n - p0, acc, w, wo, x, xo, rings[wave], wave % SPLIT, blocks, SPLIT, a.H, lane);
+            // the gate weight goes in before the rounding to bf16: one rounding of the product of both
+            if constexpr (SPLIT == 1) {
+                const int ii = i0 + (lane >> 4) * 4;   // four rows of one token
+                float bias[G][4];
 #pragma unroll
                 for (int g = 0; g < G; ++g)
-                    *(f32x4*)((float*)rings[wave] + g * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[g][jt];
-                __syncthreads();
-                const int pos = p0 + jt * 16 + (threadIdx.x >> 4), ii = i0 + (threadIdx.x & 15);
-                if (pos < n && ii < a.inner) {
-                    float v[G];
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        v[g] = a.b_up ? load_bias(a.b_up, e * a.b_up_stride + ii + g * a.inner, a.b_up_f32) : 0.0f;
+                    for (int r = 0; r < 4; ++r) bias[g][r] = a.b_up && ii < a.inner ? load_bias(a.b_up, e * a.b_up_stride + ii + r + g * a.inner, a.b_up_f32) : 0.0f;
 #pragma unroll
-                        for (int q = 0; q < kUpWaves; ++q) v[g] += ((const float*)rings[q])[g * 256 + threadIdx.x];
+                for (int jt = 0; jt < kGroups; ++jt) {
+                    const int pos = p0 + jt * 16 + (lane & 15);
+                    if (pos >= n || ii >= a.inner) continue;
+                    float h[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        h[r] = activate(a.act, acc[0][jt][r] + bias[0][r]);
+                        if (G == 2) h[r] *= acc[G - 1][jt][r] + bias[G - 1][r];
+                        h[r] *= s_gate[pos];
                     }
-                    float h = activate(a.act, v[0]);
-                    if (G == 2) h *= v[G - 1];
-                    // the gate weight goes in before the rounding to bf16: one rounding of the product of both
-                    mid[(int64_t)s_row[pos] * a.inner + ii] = (uint16_t)pack2_bf16(h * s_gate[pos], 0.0f);
+                    *(uint2*)(mid + (int64_t)s_row[pos] * a.inner + ii) = make_uint2(pack2_bf16(h[0], h[1]), pack2_bf16(h[2], h[3]));
                 }
-                __syncthreads();
+            } else {
+#pragma unroll
+                for (int jt = 0; jt < kGroups; ++jt) {
+                    if (p0 + jt * 16 >= n) break;
+#pragma unroll
+                    for (int g = 0; g < G; ++g)
+                        *(f32x4*)((float*)rings[wave] + g * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[g][jt];
+                    __syncthreads();
+                    const int pos = p0 + jt * 16 + (threadIdx.x >> 4), ii = i0 + (threadIdx.x & 15);
+                    if (pos < n && ii < a.inner) {
+                        float v[G];
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            v[g] = a.b_up ? load_bias(a.b_up, e * a.b_up_stride + ii + g * a.inner, a.b_up_f32) : 0.0f;
+#pragma unroll
+                            for (int q = 0; q < kUpWaves; ++q) v[g] += ((const float*)rings[q])[g * 256 + threadIdx.x];
+                        }
+                        float h = activate(a.act, v[0]);
+                        if (G == 2) h *= v[G - 1];
+                        mid[(int64_t)s_row[pos] * a.inner + ii] = (uint16_t)pack2_bf16(h * s_gate[pos], 0.0f);
+                    }
+                    __syncthreads();
+                }
             }
         }
     }
 }
 
+// ROWS: columns of the output per workgroup, 16 or 8 (the other half of each instruction idle).
+template <int ROWS, bool NT>
 __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const LayerArgs a, const LayerPlan plan) {
     // each wavefront's ring of weights, its part of the output [T][16], then the sorted entries
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     float* sums = (float*)(lds + kDownWaves * kDownDepth * kWeightBlock);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int h0 = blockIdx.x * kRows;
+    const int h0 = blockIdx.x * ROWS;
     int32_t* words = (int32_t*)(sums + kDownWaves * a.T * 16);
     for (int i = threadIdx.x; i < (int)sorted_words(plan.slots, a.T * a.K); i += 64 * kDownWaves) words[i] = ((const int32_t*)a.workspace)[i];
     for (int i = threadIdx.x; i < kDownWaves * a.T * 16; i += 64 * kDownWaves) sums[i] = 0.0f;
@@ -325,7 +353,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     const int64_t end = items * (wave + 1) / kDownWaves;
     char* ring = lds + wave * (kDownDepth * kWeightBlock);
     uint32_t wo[2];
-    weight_offsets(wo, a.down_row, a.H - h0, lane);
+    weight_offsets(wo, a.down_row, min(ROWS, a.H - h0), lane);
     while (q < end) {
         const int slot = (int)(q / blocks), b0 = (int)(q - (int64_t)slot * blocks);
         const int b1 = (int)min((int64_t)blocks, b0 + (end - q));
@@ -341,11 +369,11 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
                 xo[jt] = pos < n ? (uint32_t)(table.entry[first + pos] & 0xffff) * (uint32_t)a.inner * 2 : kNowhere;
                 acc[0][jt] = f32x4{0, 0, 0, 0};
             }
-            multiply_groups<1, kDownDepth>(n - p0, acc, w, wo, x, xo, ring, b0, b1, 1, a.inner, lane);
+            multiply_groups<1, kDownDepth, ROWS, NT>(n - p0, acc, w, wo, x, xo, ring, b0, b1, 1, a.inner, lane);
 #pragma unroll
             for (int jt = 0; jt < kGroups; ++jt) {
                 const int pos = p0 + jt * 16 + (lane & 15);
-                if (pos < n) {
+                if (pos < n && (lane >> 4) * 4 < ROWS) {
                     f32x4* to = (f32x4*)(mine + (table.entry[first + pos] >> 16) * 16 + (lane >> 4) * 4);
                     *to = *to + acc[0][jt];
                 }
@@ -356,7 +384,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     __syncthreads();
     for (int i = threadIdx.x; i < a.T * 16; i += 64 * kDownWaves) {
         const int t = i >> 4, c = h0 + (i & 15);
-        if (c >= a.H) continue;
+        if ((i & 15) >= ROWS || c >= a.H) continue;
         float v = 0.0f;
         for (int p = 0; p < kDownWaves; ++p) v += sums[p * a.T * 16 + i];
         if (a.b_down)
@@ -389,14 +417,36 @@ hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
     LayerPlan plan;
     plan_layer(a.T, a.K, a.L, a.H, a.inner, &plan);
     const int cus = compute_units();
-    // up: two workgroups share a compute unit; beyond four for each a workgroup takes several runs of rows, which spares
-    // the search for its expert's tokens
+    // Whole lines of weights: rows that start on lines.  A line that two blocks share would be fetched twice.
+    auto lines = [](const void* p, int64_t expert, int64_t row) { return (uintptr_t)p % 128 == 0 && expert % 64 == 0 && row % 64 == 0; };
+    // up: two workgroups share a compute unit.  Where there are runs of rows for all their wavefronts, each takes runs of its
+    // own and no sums are joined; beyond twice as many it takes several, which spares the search for its expert's tokens.
     const int slices = (a.inner + kRows - 1) / kRows;
-    plan.up_parts = std::clamp((4 * cus + plan.slots - 1) / plan.slots, 1, slices);
-    const dim3 grid((uint32_t)(plan.slots * plan.up_parts + 1));
-    if (a.gated) hipLaunchKernelGGL(layer_up_kernel<2>, grid, dim3(64 * kUpWaves), 0, s, a, plan);
-    else hipLaunchKernelGGL(layer_up_kernel<1>, grid, dim3(64 * kUpWaves), 0, s, a, plan);
-    hipLaunchKernelGGL(layer_down_kernel, dim3((uint32_t)((a.H + kRows - 1) / kRows)), dim3(64 * kDownWaves), down_lds(a.T, a.K, plan.slots), s, a, plan);
+    const bool split = (int64_t)plan.slots * slices < 2 * kUpWaves * (int64_t)cus;
+    const int runs = split ? slices : (slices + kUpWaves - 1) / kUpWaves;
+    plan.up_parts = std::clamp((4 * cus + plan.slots - 1) / plan.slots, 1, runs);
+    const dim3 grid((uint32_t)(plan.slots * plan.up_parts + 1)), block(64 * kUpWaves);
+    auto up = [&](auto g, auto n) {
+        constexpr int G = decltype(g)::value, S = decltype(n)::value;
+        if (lines(a.w_up, a.up_expert, a.up_row) && (!a.gated || a.inner * a.up_row % 64 == 0)) hipLaunchKernelGGL((layer_up_kernel<G, S, true>), grid, block, 0, s, a, plan);
+        else hipLaunchKernelGGL((layer_up_kernel<G, S, false>), grid, block, 0, s, a, plan);
+    };
+    using one = std::integral_constant<int, 1>;
+    using two = std::integral_constant<int, 2>;
+    using four = std::integral_constant<int, 4>;
+    if (a.gated) split ? up(two(), four()) : up(two(), one());
+    else split ? up(one(), four()) : up(one(), one());
+    // down: 8 columns per workgroup where 16 would leave compute units without one
+    const bool narrow = (a.H + 15) / 16 < cus;
+    const dim3 columns((uint32_t)(narrow ? (a.H + 7) / 8 : (a.H + 15) / 16));
+    const size_t lds = (size_t)down_lds(a.T, a.K, plan.slots);
+    auto down = [&](auto rows) {
+        constexpr int ROWS = decltype(rows)::value;
+        if (lines(a.w_down, a.down_expert, a.down_row)) hipLaunchKernelGGL((layer_down_kernel<ROWS, true>), columns, dim3(64 * kDownWaves), lds, s, a, plan);
+        else hipLaunchKernelGGL((layer_down_kernel<ROWS, false>), columns, dim3(64 * kDownWaves), lds, s, a, plan);
+    };
+    if (narrow) down(std::integral_constant<int, 8>());
+    else down(std::integral_constant<int, 16>());
     return hipGetLastError();
 }
 
