@@ -123,6 +123,76 @@ __device__ __forceinline__ void multiply(f32x4 (&acc)[G][kGroups], const __amdgp
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing writes to the ring any more
 }
 
+// The same for up to 16 tokens and several runs of `blocks` blocks one after the other, without a pause between them: items
+// [q0, q1) count blocks, item q is block q % blocks of run q / blocks.  open(run, w, xo) points at a run's weights and
+// rows, close(run, acc) takes its sums (of what lies in [q0, q1)).
+template <int G, int DEPTH, int ROWS, bool NT, class Open, class Close>
+__device__ __forceinline__ void stream(int64_t q0, int64_t q1, int blocks, const uint32_t (&wo)[2], __amdgpu_buffer_rsrc_t x, char* ring, int K,
+                                       int lane, Open open, Close close) {
+    constexpr int kHalves = ROWS / 8, kLoads = kHalves * G + 2;
+    if (q0 >= q1) return;
+    __amdgpu_buffer_rsrc_t w[G];
+    uint32_t xo;
+    bf16x8 xf[DEPTH][2];
+    const int wk = ((lane & 7) ^ (lane >> 3)) * 8, xk = (lane >> 4) * 8;
+    int run = (int)(q0 / blocks), b = (int)(q0 - (int64_t)run * blocks);   // of the item to multiply next
+    int run_ahead = run, b_ahead = b;                                      // and to load next
+    int to_load = (int)(q1 - q0);
+    open(run, w, xo);
+    auto load = [&](int d) {
+        if (b_ahead == blocks && to_load > 0) {
+            b_ahead = 0;
+            open(++run_ahead, w, xo);
+        }
+        const int left = to_load > 0 ? K - b_ahead * kBlock : 0;
+        const uint32_t out = wk < left ? 0 : kNowhere;   // an offset with this bit is beyond the buffer's end
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int s = 0; s < kHalves; ++s)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(w[g], (lds_ptr)(ring + (d * G + g) * kWeightBlock + s * 1024), 16,
+                                                         (wo[s] + b_ahead * (kBlock * 2)) | out, 0, 0, NT ? kNonTemporal : 0);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            xf[d][s] = load8(x, (xo + (b_ahead * kBlock + s * 32 + xk) * 2) | (s * 32 + xk < left ? 0 : kNowhere));
+        ++b_ahead;
+        --to_load;
+    };
+    const char* mine = ring + (lane & 15) * 128;
+    f32x4 acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) acc[g] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(d);
+    for (int left = (int)(q1 - q0); left > 0;) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            if (left <= 0) break;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * kLoads) : "memory");
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    const bf16x8 wf = *(const bf16x8*)(mine + (d * G + g) * kWeightBlock + (((s * 4 + (lane >> 4)) ^ (lane & 7)) << 4));
+                    acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[d][s], acc[g], 0, 0, 0);
+                }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the block has been read before its place is loaded again
+            __builtin_amdgcn_sched_barrier(0);
+            load(d);
+            --left;
+            if (++b == blocks || left == 0) {
+                close(run, acc);
+#pragma unroll
+                for (int g = 0; g < G; ++g) acc[g] = f32x4{0, 0, 0, 0};
+                ++run;
+                b = 0;
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing writes to the ring any more
+}
+
 // By the number of tokens: the more groups, the fewer blocks of them fit the registers.
 template <int G, int DEPTH, int ROWS, bool NT>
 __device__ __forceinline__ void multiply_groups(int n, f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
@@ -262,15 +332,46 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
     uint16_t* mid = (uint16_t*)(a.workspace + plan.mid);
     const int blocks = (a.H + kBlock - 1) / kBlock;
     const int slices = (a.inner + kRows - 1) / kRows;
+    // Four sums of one token (position pos of the list), rows i0 + 4 (lane / 16) on, to the workspace.  The gate weight goes
+    // in before the rounding to bf16: one rounding of the product of both.
+    auto finish = [&](int i0, int pos, const f32x4 (&sum)[G]) {
+        const int ii = i0 + (lane >> 4) * 4;
+        if (pos >= n || ii >= a.inner) return;
+        float h[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float v[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) v[g] = sum[g][r] + (a.b_up ? load_bias(a.b_up, e * a.b_up_stride + ii + r + g * a.inner, a.b_up_f32) : 0.0f);
+            h[r] = activate(a.act, v[0]);
+            if (G == 2) h[r] *= v[G - 1];
+            h[r] *= s_gate[pos];
+        }
+        *(uint2*)(mid + (int64_t)s_row[pos] * a.inner + ii) = make_uint2(pack2_bf16(h[0], h[1]), pack2_bf16(h[2], h[3]));
+    };
+    auto weights_of = [&](int i0, __amdgpu_buffer_rsrc_t (&w)[G]) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) w[g] = buffer(a.w_up + e * a.up_expert + (int64_t)(i0 + g * a.inner) * a.up_row);
+    };
     constexpr int kRuns = kUpWaves / SPLIT;   // of rows, next to each other
-    for (int slice = part * kRuns + wave / SPLIT; slice - wave / SPLIT < slices; slice += plan.up_parts * kRuns) {
+    const int first = part * kRuns + wave / SPLIT, pitch = plan.up_parts * kRuns;
+    if (SPLIT == 1 && n <= 16 && a.inner % kRows == 0) {
+        uint32_t wo[2];
+        weight_offsets(wo, a.up_row, kRows, lane);
+        const int mine = first < slices ? (slices - first + pitch - 1) / pitch : 0;
+        const uint32_t xo = (lane & 15) < n ? (uint32_t)(s_token[lane & 15] * a.x_stride * 2) : kNowhere;
+        stream<G, kUpDepth, kRows, NT>(0, (int64_t)mine * blocks, blocks, wo, x, rings[wave], a.H, lane,
+            [&](int run, __amdgpu_buffer_rsrc_t (&w)[G], uint32_t& row) { weights_of((first + run * pitch) * kRows, w); row = xo; },
+            [&](int run, const f32x4 (&acc)[G]) { finish((first + run * pitch) * kRows, lane & 15, acc); });
+        return;
+    }
+    for (int slice = first; slice - wave / SPLIT < slices; slice += pitch) {
         if (SPLIT == 1 && slice >= slices) break;
         const int i0 = slice * kRows;
         uint32_t wo[2];
         weight_offsets(wo, a.up_row, a.inner - i0, lane);
         __amdgpu_buffer_rsrc_t w[G];
-#pragma unroll
-        for (int g = 0; g < G; ++g) w[g] = buffer(a.w_up + e * a.up_expert + (int64_t)(i0 + g * a.inner) * a.up_row);
+        weights_of(i0, w);
         for (int p0 = 0; p0 < n; p0 += kGroups * 16) {
             uint32_t xo[kGroups];
             f32x4 acc[G][kGroups];
@@ -282,49 +383,26 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
                 for (int g = 0; g < G; ++g) acc[g][jt] = f32x4{0, 0, 0, 0};
             }
             multiply_groups<G, kUpDepth, kRows, NT>(n - p0, acc, w, wo, x, xo, rings[wave], wave % SPLIT, blocks, SPLIT, a.H, lane);
-            // the gate weight goes in before the rounding to bf16: one rounding of the product of both
-            if constexpr (SPLIT == 1) {
-                const int ii = i0 + (lane >> 4) * 4;   // four rows of one token
-                float bias[G][4];
 #pragma unroll
-                for (int g = 0; g < G; ++g)
+            for (int jt = 0; jt < kGroups; ++jt) {
+                if (p0 + jt * 16 >= n) break;
+                f32x4 sum[G];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) bias[g][r] = a.b_up && ii < a.inner ? load_bias(a.b_up, e * a.b_up_stride + ii + r + g * a.inner, a.b_up_f32) : 0.0f;
+                for (int g = 0; g < G; ++g) sum[g] = acc[g][jt];
+                if constexpr (SPLIT > 1) {   // wavefront 0 adds the others' parts to its own, in order
 #pragma unroll
-                for (int jt = 0; jt < kGroups; ++jt) {
-                    const int pos = p0 + jt * 16 + (lane & 15);
-                    if (pos >= n || ii >= a.inner) continue;
-                    float h[4];
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        h[r] = activate(a.act, acc[0][jt][r] + bias[0][r]);
-                        if (G == 2) h[r] *= acc[G - 1][jt][r] + bias[G - 1][r];
-                        h[r] *= s_gate[pos];
-                    }
-                    *(uint2*)(mid + (int64_t)s_row[pos] * a.inner + ii) = make_uint2(pack2_bf16(h[0], h[1]), pack2_bf16(h[2], h[3]));
-                }
-            } else {
-#pragma unroll
-                for (int jt = 0; jt < kGroups; ++jt) {
-                    if (p0 + jt * 16 >= n) break;
-#pragma unroll
-                    for (int g = 0; g < G; ++g)
-                        *(f32x4*)((float*)rings[wave] + g * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[g][jt];
+                    for (int g = 0; g < G; ++g) *(f32x4*)((float*)rings[wave] + (g * 64 + lane) * 4) = sum[g];
                     __syncthreads();
-                    const int pos = p0 + jt * 16 + (threadIdx.x >> 4), ii = i0 + (threadIdx.x & 15);
-                    if (pos < n && ii < a.inner) {
-                        float v[G];
+                    if (wave == 0) {
 #pragma unroll
-                        for (int g = 0; g < G; ++g) {
-                            v[g] = a.b_up ? load_bias(a.b_up, e * a.b_up_stride + ii + g * a.inner, a.b_up_f32) : 0.0f;
+                        for (int g = 0; g < G; ++g)
 #pragma unroll
-                            for (int q = 0; q < kUpWaves; ++q) v[g] += ((const float*)rings[q])[g * 256 + threadIdx.x];
-                        }
-                        float h = activate(a.act, v[0]);
-                        if (G == 2) h *= v[G - 1];
-                        mid[(int64_t)s_row[pos] * a.inner + ii] = (uint16_t)pack2_bf16(h * s_gate[pos], 0.0f);
+                            for (int q = 1; q < SPLIT; ++q) sum[g] += *(const f32x4*)((const float*)rings[q] + (g * 64 + lane) * 4);
+                        finish(i0, p0 + jt * 16 + (lane & 15), sum);
                     }
                     __syncthreads();
+                } else {
+                    finish(i0, p0 + jt * 16 + (lane & 15), sum);
                 }
             }
         }
@@ -354,6 +432,24 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     char* ring = lds + wave * (kDownDepth * kWeightBlock);
     uint32_t wo[2];
     weight_offsets(wo, a.down_row, min(ROWS, a.H - h0), lane);
+    int most = 0;   // entries of one expert
+    for (int i = lane; i < *table.count; i += 64) most = max(most, table.start[i + 1] - table.start[i]);
+    if (!__any(most > 16)) {
+        stream<1, kDownDepth, ROWS, NT>(q, end, blocks, wo, x, ring, a.inner, lane,
+            [&](int slot, __amdgpu_buffer_rsrc_t (&w)[1], uint32_t& row) {
+                const int e = __builtin_amdgcn_readfirstlane(table.expert[slot]), pos = table.start[slot] + (lane & 15);
+                w[0] = buffer(a.w_down + e * a.down_expert + (int64_t)h0 * a.down_row);
+                row = pos < table.start[slot + 1] ? (uint32_t)(table.entry[pos] & 0xffff) * (uint32_t)a.inner * 2 : kNowhere;
+            },
+            [&](int slot, const f32x4 (&acc)[1]) {
+                const int pos = table.start[slot] + (lane & 15);
+                if (pos < table.start[slot + 1] && (lane >> 4) * 4 < ROWS) {
+                    f32x4* to = (f32x4*)(mine + (table.entry[pos] >> 16) * 16 + (lane >> 4) * 4);
+                    *to = *to + acc[0];
+                }
+            });
+        q = end;
+    }
     while (q < end) {
         const int slot = (int)(q / blocks), b0 = (int)(q - (int64_t)slot * blocks);
         const int b1 = (int)min((int64_t)blocks, b0 + (end - q));
