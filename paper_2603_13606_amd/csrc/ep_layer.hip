@@ -124,25 +124,24 @@ __device__ __forceinline__ void multiply(f32x4 (&acc)[G][kGroups], const __amdgp
 }
 
 // The same for up to 16 tokens and several runs of `blocks` blocks one after the other, without a pause between them: items
-// [q0, q1) count blocks, item q is block q % blocks of run q / blocks.  open(run, w, xo) points at a run's weights and
+// [q0, q1) count blocks, item q is block q % blocks of run q / blocks.  open(run, w, wo, xo) points at a run's weights and
 // rows, close(run, acc) takes its sums (of what lies in [q0, q1)).
 template <int G, int DEPTH, int ROWS, bool NT, class Open, class Close>
-__device__ __forceinline__ void stream(int64_t q0, int64_t q1, int blocks, const uint32_t (&wo)[2], __amdgpu_buffer_rsrc_t x, char* ring, int K,
-                                       int lane, Open open, Close close) {
+__device__ __forceinline__ void stream(int64_t q0, int64_t q1, int blocks, __amdgpu_buffer_rsrc_t x, char* ring, int K, int lane, Open open, Close close) {
     constexpr int kHalves = ROWS / 8, kLoads = kHalves * G + 2;
     if (q0 >= q1) return;
     __amdgpu_buffer_rsrc_t w[G];
-    uint32_t xo;
+    uint32_t wo[2], xo;
     bf16x8 xf[DEPTH][2];
     const int wk = ((lane & 7) ^ (lane >> 3)) * 8, xk = (lane >> 4) * 8;
     int run = (int)(q0 / blocks), b = (int)(q0 - (int64_t)run * blocks);   // of the item to multiply next
     int run_ahead = run, b_ahead = b;                                      // and to load next
     int to_load = (int)(q1 - q0);
-    open(run, w, xo);
+    open(run, w, wo, xo);
     auto load = [&](int d) {
         if (b_ahead == blocks && to_load > 0) {
             b_ahead = 0;
-            open(++run_ahead, w, xo);
+            open(++run_ahead, w, wo, xo);
         }
         const int left = to_load > 0 ? K - b_ahead * kBlock : 0;
         const uint32_t out = wk < left ? 0 : kNowhere;   // an offset with this bit is beyond the buffer's end
@@ -212,16 +211,16 @@ __device__ __forceinline__ void weight_offsets(uint32_t (&wo)[2], int64_t stride
     }
 }
 
-// The routed entries sorted by expert, by one workgroup.  The order of an expert's entries is arbitrary: each token's
-// column is a sum of its own.
-__device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan& plan, int* fill) {
+// The routed entries sorted by expert, by one workgroup, from their local ids.  The order of an expert's entries is
+// arbitrary: each token's column is a sum of its own.
+__device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan& plan, const int16_t* ids, int* fill) {
     const Sorted out = sorted_at(a.workspace, plan.slots);
     for (int e = threadIdx.x; e < kMaxExperts; e += 64 * kUpWaves) fill[e] = 0;
     __syncthreads();
-    auto entry_id = [&](int i) {
-        const int t = i / a.K, k = i - t * a.K, e = local_id(a, t, k);
-        for (int q = 0; q < k && e >= 0; ++q)
-            if (local_id(a, t, q) == e) return -1;
+    auto entry_id = [&](int i) {   // -1 for the second entry of a token that names the same expert, too
+        const int e = ids[i];
+        for (int q = i - i % a.K; q < i && e >= 0; ++q)
+            if (ids[q] == e) return -1;
         return e;
     };
     for (int i = threadIdx.x; i < a.T * a.K; i += 64 * kUpWaves) {
@@ -232,10 +231,12 @@ __device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan
     if (threadIdx.x < 64) {
         constexpr int kPer = kMaxExperts / 64;
         const int lane = threadIdx.x, e0 = lane * kPer;
-        int sum = 0, named = 0;
-        for (int e = e0; e < e0 + kPer; ++e) {
-            sum += fill[e];
-            named += fill[e] > 0;
+        int n[kPer], sum = 0, named = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            n[i] = fill[e0 + i];
+            sum += n[i];
+            named += n[i] > 0;
         }
         int s1 = sum, n1 = named;
 #pragma unroll
@@ -244,14 +245,14 @@ __device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan
             if (lane >= d) { s1 += v; n1 += u; }
         }
         int at = s1 - sum, slot = n1 - named;
-        for (int e = e0; e < e0 + kPer; ++e) {
-            const int n = fill[e];
-            fill[e] = at;
-            if (n > 0) {
-                out.expert[slot] = e;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            fill[e0 + i] = at;
+            if (n[i] > 0) {
+                out.expert[slot] = e0 + i;
                 out.start[slot] = at;
                 ++slot;
-                at += n;
+                at += n[i];
             }
         }
         if (lane == 63) {
@@ -276,20 +277,23 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
     __shared__ int s_token[kLayerMaxTokens], s_row[kLayerMaxTokens];
     __shared__ float s_gate[kLayerMaxTokens];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int16_t* ids = (int16_t*)rings;   // local ids of all entries, until the weights come
+    static_assert(sizeof(rings) >= 2 * kLayerMaxTokens * kMaxTopK + 4 * kMaxExperts, "ids and the sort's counters");
+    if (threadIdx.x < kMaxExperts / 32) named[threadIdx.x] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.T * a.K; i += 64 * kUpWaves) {
+        const int e = local_id(a, i / a.K, i % a.K);
+        ids[i] = (int16_t)e;
+        if (e >= 0) atomicOr(&named[e >> 5], 1u << (e & 31));
+    }
+    __syncthreads();
     if (blockIdx.x == 0) {
-        sort_entries(a, plan, (int*)rings);
+        sort_entries(a, plan, ids, (int*)(ids + kLayerMaxTokens * kMaxTopK));
         return;
     }
     const int slot = (blockIdx.x - 1) / plan.up_parts, part = (blockIdx.x - 1) % plan.up_parts;
 
     // the slot-th of the experts that any token names
-    if (threadIdx.x < kMaxExperts / 32) named[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.T * a.K; i += 64 * kUpWaves) {
-        const int e = local_id(a, i / a.K, i % a.K);
-        if (e >= 0) atomicOr(&named[e >> 5], 1u << (e & 31));
-    }
-    __syncthreads();
     const uint32_t word = lane < kMaxExperts / 32 ? named[lane] : 0u;
     int upto = __popc(word);
 #pragma unroll
@@ -310,7 +314,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
     if ((int)threadIdx.x < a.T) {
         const int t = threadIdx.x;
         for (int k = 0; k < a.K; ++k)
-            if (local_id(a, t, k) == e) {
+            if (ids[t * a.K + k] == e) {
                 if (!has) row = t * a.K + k;
                 has = true;
                 gate += a.topk_w ? a.topk_w[t * a.w_stride + k] : 1.0f;
@@ -326,7 +330,7 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
         s_row[pos] = row;
         s_gate[pos] = gate;
     }
-    __syncthreads();
+    __syncthreads();   // the ids have been read, too: weights may take their place
 
     const auto x = buffer(a.x);
     uint16_t* mid = (uint16_t*)(a.workspace + plan.mid);
@@ -355,13 +359,16 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
     };
     constexpr int kRuns = kUpWaves / SPLIT;   // of rows, next to each other
     const int first = part * kRuns + wave / SPLIT, pitch = plan.up_parts * kRuns;
-    if (SPLIT == 1 && n <= 16 && a.inner % kRows == 0) {
-        uint32_t wo[2];
-        weight_offsets(wo, a.up_row, kRows, lane);
+    if (SPLIT == 1 && n <= 16) {
         const int mine = first < slices ? (slices - first + pitch - 1) / pitch : 0;
         const uint32_t xo = (lane & 15) < n ? (uint32_t)(s_token[lane & 15] * a.x_stride * 2) : kNowhere;
-        stream<G, kUpDepth, kRows, NT>(0, (int64_t)mine * blocks, blocks, wo, x, rings[wave], a.H, lane,
-            [&](int run, __amdgpu_buffer_rsrc_t (&w)[G], uint32_t& row) { weights_of((first + run * pitch) * kRows, w); row = xo; },
+        stream<G, kUpDepth, kRows, NT>(0, (int64_t)mine * blocks, blocks, x, rings[wave], a.H, lane,
+            [&](int run, __amdgpu_buffer_rsrc_t (&w)[G], uint32_t (&wo)[2], uint32_t& row) {
+                const int i0 = (first + run * pitch) * kRows;
+                weights_of(i0, w);
+                weight_offsets(wo, a.up_row, a.inner - i0, lane);
+                row = xo;
+            },
             [&](int run, const f32x4 (&acc)[G]) { finish((first + run * pitch) * kRows, lane & 15, acc); });
         return;
     }
@@ -435,8 +442,10 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     int most = 0;   // entries of one expert
     for (int i = lane; i < *table.count; i += 64) most = max(most, table.start[i + 1] - table.start[i]);
     if (!__any(most > 16)) {
-        stream<1, kDownDepth, ROWS, NT>(q, end, blocks, wo, x, ring, a.inner, lane,
-            [&](int slot, __amdgpu_buffer_rsrc_t (&w)[1], uint32_t& row) {
+        stream<1, kDownDepth, ROWS, NT>(q, end, blocks, x, ring, a.inner, lane,
+            [&](int slot, __amdgpu_buffer_rsrc_t (&w)[1], uint32_t (&to)[2], uint32_t& row) {
+                to[0] = wo[0];
+                to[1] = wo[1];
                 const int e = __builtin_amdgcn_readfirstlane(table.expert[slot]), pos = table.start[slot] + (lane & 15);
                 w[0] = buffer(a.w_down + e * a.down_expert + (int64_t)h0 * a.down_row);
                 row = pos < table.start[slot + 1] ? (uint32_t)(table.entry[pos] & 0xffff) * (uint32_t)a.inner * 2 : kNowhere;
