@@ -42,6 +42,7 @@ struct Product {
     int64_t out_expert, out_row;
     int I, J, Kc;        // extents along P, along Q (grad_W) and of the contraction (not grad_W)
     // forward
+    int p_lines;         // rows of the weights start on 128-byte lines
     int act, gated;
     const void* bias;
     int64_t bias_stride;
@@ -122,17 +123,27 @@ __device__ __forceinline__ int find_expert(const int* starts, int L, int b) {
 
 constexpr int kPanel = 64 * kBK * 2;
 
+// A value that is the same in all lanes, where the compiler does not see that.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
+    const uint64_t b = (uint64_t)p;
+    const uint64_t at = (uint64_t)(uint32_t)uniform((int)(b >> 32)) << 32 | (uint32_t)uniform((int)b);
+    return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, 0x7fffffff, 0x00027000);
+}
+
 __device__ __forceinline__ int spread(int k) { return ((k >> 1) & 1) | ((k >> 2) & 2); }
 
 // Sixteen bytes per lane from the buffer to LDS, lane after lane from the wave's address on.  Written in assembly, which
 // has no output register: the compiler puts a wait for all such loads in front of every transposing LDS read when it
 // knows of them, and would let none of them run ahead.  The waits are the caller's.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, uint32_t offset) {
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, uint32_t offset, bool once = false) {
     const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr)lds;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(rsrc) : "memory");
+    if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(at), "v"(offset), "s"(rsrc) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(rsrc) : "memory");
 }
 
-template <int B, bool KM, int NW>
+template <int B, bool KM, int NW, bool HINT>
 struct Operand {
     static constexpr int kLoads = B / 64 * 8 / NW;   // of 8 rows each, per wavefront
     static constexpr int kBytes = B * kBK * 2;
@@ -140,6 +151,7 @@ struct Operand {
     const uint16_t* base;     // of the next contraction step to load
     int64_t step;             // elements per contraction step
     int k0;                   // contraction index of the lane's first unit (KM: the same in every load)
+    int once = 0;             // HINT: nobody else reads this tile, and it comes in whole lines: the non-temporal hint pays
 
     // rows_of(r): the source row of tile row r relative to base, or -1
     template <class F>
@@ -170,12 +182,13 @@ struct Operand {
     // Loads [j0, j1) of the tile of the current step; `left` = contraction indices that remain there.
     template <int J0, int J1>
     __device__ __forceinline__ void load(char* lds, int left, int wave) {
-        auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, 0x7fffffff, 0x00027000);
+        const auto rsrc = buffer(base);
+        const bool hint = HINT && uniform(once);
 #pragma unroll
         for (int j = J0; j < J1; ++j) {
             const int k = KM ? k0 : k0 + ((j * NW + wave) & 7) * 8;
             const uint32_t o = k < left ? off[j] : kNowhere;
-            load_to_lds(rsrc, lds + (j * NW + wave) * 1024, o);
+            load_to_lds(rsrc, lds + (j * NW + wave) * 1024, o, hint);
         }
     }
     __device__ __forceinline__ void next() { base += step; }
@@ -216,9 +229,6 @@ __device__ __forceinline__ int opaque(int v) {
 }
 
 // Accesses of results: a lane that has nothing there reads zeros and writes nothing (offset kNowhere).
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t results(const void* p) {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, 0x7fffffff, 0x00027000);
-}
 __device__ __forceinline__ f32x4 load4(__amdgpu_buffer_rsrc_t r, uint32_t off, int is_f32) {
     if (is_f32) return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
     return widen(__builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0)));
@@ -257,11 +267,12 @@ __device__ __forceinline__ bool narrow_tiles(int64_t blocks, int width, int work
 template <int KIND, int BI>
 __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table) {
     constexpr int BJ = kBJ, NW = kWaves;
-    constexpr bool PHASED = BI == 256;
+    constexpr bool WIDE = BI == 256;
     constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
     constexpr int WI = BI / NWI, WJ = BJ / NWJ, IT = WI / 16, JT = WJ / 16;
-    using P = Operand<BI, kPK, NW>;
-    using Q = Operand<BJ, kQK, NW>;
+    constexpr bool kHint = BI == 128 && KIND != GRAD_WEIGHTS;
+    using P = Operand<BI, kPK, NW, kHint>;
+    using Q = Operand<BJ, kQK, NW, false>;
     constexpr int kStage = P::kBytes + Q::kBytes;
     constexpr int kLoads = P::kLoads + Q::kLoads;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -279,7 +290,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     // Workgroups of one XCD (blockIdx mod 8) take neighbouring tiles, so that its L2 serves both operands.
     struct Tile {
         int e, i0, j0, rows, first;
-        bool first_i;
+        int first_i, alone;    // the first block along I; the only one along J of its expert
     };
     auto locate = [&](int64_t t) {
         Tile c;
@@ -293,6 +304,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         c.j0 = __builtin_amdgcn_readfirstlane(band * 8 + in - ib * height) * BJ;
         c.i0 = ib * bi;
         c.first_i = ib == 0;
+        c.alone = m == 1;
         c.rows = __builtin_amdgcn_readfirstlane(table->rows[c.e]);
         c.first = __builtin_amdgcn_readfirstlane(table->first[c.e]);
         return c;
@@ -304,6 +316,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     auto begin = [&](const Tile& c) {
         const int lane = opaque(threadIdx.x & 63);
         const uint16_t* pb = a.p + c.e * a.p_expert;
+        if (kHint) p.once = c.alone && a.p_lines;
         if constexpr (KIND == FORWARD) {
             const int I = a.I, gated = a.gated, i0 = c.i0;
             p.start_rows(pb + c.i0 * a.p_row, a.p_row, wave, lane, [=](int r) {
@@ -325,7 +338,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             p.template load<0, P::kLoads>(lds, Kc, wave);
             q.template load<0, Q::kLoads>(lds + P::kBytes, Kc, wave);
             p.next(); q.next();
-            if constexpr (PHASED) {
+            if constexpr (WIDE) {
                 if (Kc > kBK) {
                     p.template load<0, 1>(lds + kStage, Kc - kBK, wave);
                     p.template load<2, 3>(lds + kStage, Kc - kBK, wave);
@@ -348,7 +361,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     if (t >= tiles) return;
     Tile c = locate(t);
     begin(c);
-    bool fresh = true;   // no results have been stored since the tile's first loads
+    int fresh = 1;   // no results have been stored since the tile's first loads
     for (;;) {
         const int steps = steps_of(c);
         const int Kc = KIND == GRAD_WEIGHTS ? c.rows : a.Kc;
@@ -360,11 +373,13 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
 #pragma unroll
             for (int it = 0; it < IT; ++it) acc[it][jt] = f32x4{0, 0, 0, 0};
         }
-        const bool with_sums = KIND == GRAD_WEIGHTS && a.grad_b && c.first_i && wi == 0;
+        const bool with_sums = uniform(KIND == GRAD_WEIGHTS && a.grad_b && c.first_i && wi == 0);
 
         const uint32_t pl = fragment_lane<kPK>(lane), ql = fragment_lane<kQK>(lane);
+        const bool idle = !WIDE && uniform(KIND != GRAD_WEIGHTS && wj * WJ >= c.rows - c.j0);   // none of the wavefront's rows exist
+        const bool late = wave >= 4;
         const s16x8 one = {0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80, 0x3f80};
-        if constexpr (PHASED) {
+        if constexpr (WIDE) {
             // Two groups of four wavefronts, one of each per SIMD, half a phase apart: while one group multiplies, the
             // other reads fragments and issues loads.  A step has two phases, the halves of a wavefront's tile along P;
             // each is a load interval and a product interval of 32 instructions, and every interval ends in a barrier.
@@ -374,13 +389,12 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             // what the next phase reads in LDS.
             static_assert(P::kLoads == 4 && Q::kLoads == 4 && NW == 8, "");
             constexpr int IH = IT / 2;
-            const bool late = wave >= 4;
             if (steps) {
                 // Step 0 has landed when only the six loads for step 1 and the results stored since are on their way: of
                 // those at least 8 (gated) or 16 per lane.
                 if (steps == 1) {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                } else if (fresh) {
+                } else if (uniform(fresh)) {
                     asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
                 } else if (KIND == FORWARD && a.gated) {
                     asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
@@ -450,52 +464,65 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             }
             if (steps && !late) barrier();
         } else {
-            // Three stages, the loads of the step after next under way while one is multiplied, one barrier per step: it
-            // tells that everybody's part of the step's tile has landed, and that the place of the step before is free.
-            const bool idle = KIND != GRAD_WEIGHTS && wj * WJ >= c.rows - c.j0;   // none of the wavefront's rows exist
-            int stage = 0;
-            for (int k = 0; k < steps; ++k) {
-                const char* cur = lds + stage * kStage;
-                // besides the next step's loads the results stored since may be on their way at first: at least IT * JT / 2
-                // per lane (gated: half)
-                if (k + 1 >= steps) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                else if (k > 0 || fresh) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+            // The same two groups with one load interval (all fragments of a step, 64 KiB of LDS reads per group) and one
+            // product interval (32 instructions, as long) per step, and three stages: the loads of step k + 2 take the place
+            // of step k - 1, which everybody has read.
+            if (steps) {
+                // besides step 1's loads the results stored since may be on their way: at least 4 (gated) or 8 per lane
+                if (steps == 1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                else if (uniform(fresh)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
                 else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads + (KIND == FORWARD ? IT * JT / 4 : IT * JT / 2)) : "memory");
                 barrier();
+                if (late) barrier();
+            }
+            int stage = 0;
+            for (int k = 0; k < steps; ++k) {
+                const char* pc = lds + stage * kStage + wi * WI * 128;
+                const char* qc = lds + stage * kStage + P::kBytes + wj * WJ * 128;
+                bf16x8 pf[2][IT], qf[2][JT];
+                if (!idle) {
+#pragma unroll
+                    for (int it = 0; it < IT; ++it) {
+                        pf[0][it] = fragment<kPK, 0>(pc, it * 16, pl);
+                        pf[1][it] = fragment<kPK, 1>(pc, it * 16, pl);
+                    }
+#pragma unroll
+                    for (int jt = 0; jt < JT; ++jt) {
+                        qf[0][jt] = fragment<kQK, 0>(qc, jt * 16, ql);
+                        qf[1][jt] = fragment<kQK, 1>(qc, jt * 16, ql);
+                    }
+                }
                 if (k + 2 < steps) {
                     char* to = lds + (stage == 0 ? 2 : stage - 1) * kStage;
                     p.template load<0, P::kLoads>(to, Kc - (k + 2) * kBK, wave);
                     q.template load<0, Q::kLoads>(to + P::kBytes, Kc - (k + 2) * kBK, wave);
                     p.next(); q.next();
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");   // step k + 1 has landed
+                } else {
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 }
                 stage = stage == 2 ? 0 : stage + 1;
-                if (idle) continue;
-                bf16x8 pf[2][IT], qf[2][JT];
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                barrier();
+                if (!idle) {
+                    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int it = 0; it < IT; ++it) {
-                    pf[0][it] = fragment<kPK, 0>(cur + wi * WI * 128, it * 16, pl);
-                    pf[1][it] = fragment<kPK, 1>(cur + wi * WI * 128, it * 16, pl);
+                    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+                        for (int it = 0; it < IT; ++it)
+#pragma unroll
+                            for (int jt = 0; jt < JT; ++jt)
+                                acc[it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jt], acc[it][jt], 0, 0, 0);
+                        if (with_sums)
+#pragma unroll
+                            for (int jt = 0; jt < JT; ++jt)
+                                sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jt], sums[jt], 0, 0, 0);
+                    }
+                    __builtin_amdgcn_s_setprio(0);
                 }
-#pragma unroll
-                for (int jt = 0; jt < JT; ++jt) {
-                    qf[0][jt] = fragment<kQK, 0>(cur + P::kBytes + wj * WJ * 128, jt * 16, ql);
-                    qf[1][jt] = fragment<kQK, 1>(cur + P::kBytes + wj * WJ * 128, jt * 16, ql);
-                }
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks) {
-#pragma unroll
-                    for (int it = 0; it < IT; ++it)
-#pragma unroll
-                        for (int jt = 0; jt < JT; ++jt)
-                            acc[it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jt], acc[it][jt], 0, 0, 0);
-                    if (with_sums)
-#pragma unroll
-                        for (int jt = 0; jt < JT; ++jt)
-                            sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jt], sums[jt], 0, 0, 0);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // read, before the barrier of the next step says so
+                barrier();
             }
-            if (steps) barrier();
+            if (steps && !late) barrier();
         }
 
         // The next tile's first loads run while this one's results are written.
@@ -523,12 +550,12 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         const char* out = (const char*)a.out;
         if constexpr (KIND == GRAD_WEIGHTS) out += (done.e * a.out_expert + done.j0 * a.out_row + done.i0) * esize;
         else out += (done.e * a.out_expert + (done.first + done.j0) * a.out_row + done.i0) * 2;
-        const auto ro = results(out);
+        const auto ro = buffer(out);
         if constexpr (KIND == FORWARD) {
             const int nit = a.gated ? IT / 2 : IT;
             if (a.bias) {
                 const int size = a.bias_f32 ? 4 : 2;
-                const auto rb = results((const char*)a.bias + (done.e * a.bias_stride + done.i0) * size);
+                const auto rb = buffer((const char*)a.bias + (done.e * a.bias_stride + done.i0) * size);
 #pragma unroll
                 for (int it = 0; it < IT; ++it) {
                     const int i = i4 + (it < nit ? it : it - nit) * 16;
@@ -540,7 +567,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                 }
             }
             if (a.pre) {
-                const auto rp = results(a.pre + done.e * a.pre_expert + (done.first + done.j0) * a.pre_row + done.i0);
+                const auto rp = buffer(a.pre + done.e * a.pre_expert + (done.first + done.j0) * a.pre_row + done.i0);
 #pragma unroll
                 for (int it = 0; it < IT; it += 2)
 #pragma unroll
@@ -549,7 +576,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                         store8(rp, at(jt, i, a.pre_row, 2) + (it < nit || i >= Il ? 0 : a.I * 2), acc[it][jt], acc[it + 1][jt]);
                     }
             }
-            const auto rr = results(a.res + done.e * a.res_expert + (done.first + done.j0) * a.res_row + done.i0);
+            const auto rr = buffer(a.res + done.e * a.res_expert + (done.first + done.j0) * a.res_row + done.i0);
             auto finish = [&](auto activation, auto gate) {
                 constexpr int kN = decltype(gate)::value ? IT / 2 : IT;
 #pragma unroll
@@ -630,7 +657,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         }
         if (!again) return;
         t = next;
-        fresh = false;
+        fresh = 0;
     }
 }
 
@@ -729,6 +756,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     Product p = {};
     p.win = a.win;
     p.p = a.w; p.p_expert = a.w_expert; p.p_row = a.w_row;
+    p.p_lines = (uintptr_t)a.w % 128 == 0 && a.w_expert % 64 == 0 && a.w_row % 64 == 0;
     p.q = a.x.base; p.q_expert = a.x.expert_stride; p.q_row = a.x.row_stride;
     p.out = a.out.base; p.out_expert = a.out.expert_stride; p.out_row = a.out.row_stride;
     p.I = a.No; p.Kc = a.Kd;
@@ -744,6 +772,7 @@ hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
     Product p = {};
     p.win = a.win;
     p.p = a.w; p.p_expert = a.w_expert; p.p_row = a.w_row;
+    p.p_lines = (uintptr_t)a.w % 128 == 0 && a.w_expert % 64 == 0 && a.w_row % 64 == 0;
     p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
     p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
     p.I = a.Kd; p.Kc = a.N;
