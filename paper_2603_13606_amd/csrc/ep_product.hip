@@ -256,16 +256,12 @@ constexpr int kFlatStages = 3;
 // Tiles of 256 along P in two stages, or of 128 in three.
 constexpr int kLdsTiles = std::max(2 * (256 + kBJ) * kBK * 2, kFlatStages * (128 + kBJ) * kBK * 2);
 
-// Whether tiles of 128 along P take fewer rounds of the workgroups, a round of them being NARROW/WIDE as long.
-__device__ __forceinline__ bool narrow_tiles(int64_t blocks, int width, int workgroups) {
-    const int64_t wide = (blocks * ((width + 255) / 256) + workgroups - 1) / workgroups;
-    const int64_t narrow = (blocks * ((width + 127) / 128) + workgroups - 1) / workgroups;
-    return 5 * narrow < 8 * wide;
-}
+// Tiles of 256 along P that a row of tiles takes.
+__device__ __forceinline__ int wide_columns(const Product& a, int kind) { return (a.I * (kind == FORWARD && a.gated ? 2 : 1) + 255) / 256; }
 
-// All tiles of one workgroup, BI indices of P by kBJ of Q.
+// All tiles of one workgroup, BI indices of P by kBJ of Q: tiles [from, from + count) of 256 indices of P, or their halves.
 template <int KIND, int BI>
-__device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table) {
+__device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table, int64_t from, int64_t count) {
     constexpr int BJ = kBJ, NW = kWaves;
     constexpr bool WIDE = BI == 256;
     constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
@@ -278,13 +274,11 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave % NWI, wj = wave / NWI;
 
-    // Tiles: blocks of BJ rows of the experts that have rows (grad_W: of BJ weight rows, for every expert),
-    // times blocks along I.  A gated tile holds BI/2 outputs: their gate and their up columns.
+    // A gated tile holds BI/2 outputs: their gate and their up columns.
     const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
-    const int ni = (a.I + bi - 1) / bi;
+    const int ni = wide_columns(a, KIND);
     const int weight_blocks = KIND == GRAD_WEIGHTS ? (a.J + BJ - 1) / BJ : 0;
-    const int nj = KIND == GRAD_WEIGHTS ? a.win.L * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[a.win.L]);
-    const int64_t tiles = (int64_t)nj * ni;
+    const int64_t tiles = WIDE ? count : 2 * count;   // first halves, then second halves, of which the last may be empty
 
     // Tile t: expert by expert, within an expert in bands of eight row blocks, within a band column block by column block.
     // Workgroups of one XCD (blockIdx mod 8) take neighbouring tiles, so that its L2 serves both operands.
@@ -292,8 +286,10 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         int e, i0, j0, rows, first;
         int first_i, alone;    // the first block along I; the only one along J of its expert
     };
-    auto locate = [&](int64_t t) {
+    auto locate = [&](int64_t u) {
         Tile c;
+        const int half = !WIDE && u >= count;
+        const int64_t t = from + (half ? u - count : u);
         const int block = (int)(t / ni);
         c.e = __builtin_amdgcn_readfirstlane(KIND == GRAD_WEIGHTS ? block / weight_blocks : find_expert(table->starts, a.win.L, block));
         const int start = KIND == GRAD_WEIGHTS ? c.e * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[c.e]);
@@ -302,8 +298,8 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         const int band = (int)(local / (8 * ni)), height = min(8, m - band * 8), in = (int)(local - (int64_t)band * 8 * ni);
         const int ib = __builtin_amdgcn_readfirstlane(in / height);
         c.j0 = __builtin_amdgcn_readfirstlane(band * 8 + in - ib * height) * BJ;
-        c.i0 = ib * bi;
-        c.first_i = ib == 0;
+        c.i0 = ib * (WIDE ? bi : 2 * bi) + half * bi;
+        c.first_i = c.i0 == 0;
         c.alone = m == 1;
         c.rows = __builtin_amdgcn_readfirstlane(table->rows[c.e]);
         c.first = __builtin_amdgcn_readfirstlane(table->first[c.e]);
@@ -358,8 +354,16 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
 
     const int per = gridDim.x >> 3;
     int64_t t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if (t >= tiles) return;
-    Tile c = locate(t);
+    Tile c;
+    // The workgroup's next tile that is not empty, from t on.
+    auto find = [&] {
+        for (; t < tiles; t += gridDim.x) {
+            c = locate(t);
+            if (WIDE || c.i0 < a.I) return true;
+        }
+        return false;
+    };
+    if (!find()) return;
     begin(c);
     int fresh = 1;   // no results have been stored since the tile's first loads
     for (;;) {
@@ -527,12 +531,9 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
 
         // The next tile's first loads run while this one's results are written.
         const Tile done = c;
-        const int64_t next = t + gridDim.x;
-        const bool again = next < tiles;
-        if (again) {
-            c = locate(next);
-            begin(c);
-        }
+        t += gridDim.x;
+        const bool again = find();
+        if (again) begin(c);
 
         // Results: lane l holds, for index j = l % 16 of a fragment of Q, the indices i = 4 (l / 16) .. + 3 of one of P;
         // stored in pairs of fragments (store8), eight of one: i8.
@@ -656,7 +657,6 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             }
         }
         if (!again) return;
-        t = next;
         fresh = 0;
     }
 }
@@ -670,9 +670,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a
         if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
     }
     __syncthreads();
-    const int64_t blocks = KIND == GRAD_WEIGHTS ? (int64_t)a.win.L * ((a.J + kBJ - 1) / kBJ) : __builtin_amdgcn_readfirstlane(table->starts[a.win.L]);
-    if (narrow_tiles(blocks, a.I * (KIND == FORWARD && a.gated ? 2 : 1), gridDim.x)) product_tiles<KIND, 128>(a, lds, table);
-    else product_tiles<KIND, 256>(a, lds, table);
+    // Blocks of kBJ rows of the experts that have rows (grad_W: of kBJ weight rows, for every expert), times blocks along I.
+    // They go in rounds of the workgroups.  Where the last round would leave half of them without a tile it takes tiles of 128
+    // along P instead, whose steps take 5/8 of the time: all of them for small inputs, in one round.
+    const int64_t blocks = KIND == GRAD_WEIGHTS ? (int64_t)a.win.L * ((a.J + kBJ - 1) / kBJ) : uniform(table->starts[a.win.L]);
+    const int64_t tiles = blocks * wide_columns(a, KIND), rest = tiles % gridDim.x;
+    const bool halve = 2 * rest <= gridDim.x;
+    product_tiles<KIND, 256>(a, lds, table, 0, halve ? tiles - rest : tiles);
+    if (halve) product_tiles<KIND, 128>(a, lds, table, tiles - rest, rest);
 }
 
 // grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows.
