@@ -66,18 +66,25 @@ __device__ __forceinline__ int window_rows(const Windows& w, int e, int64_t* fir
     return (int)n;
 }
 
-// The windows of a call in LDS: first row and rows of each expert, starts[e] = blocks of `rows` rows before expert e,
-// starts[L] = all of them.
+// The windows of a call in LDS: first row and rows of each expert.  Its rows go in blocks of `rows`, or in one short block if
+// half of that is enough for all of them (the short end of a longer window is a block like the others: it goes next to
+// them, while the weights are in the L2; apart from them it would read the weights again, 668 against 711 us at 32 x 300 rows of
+// 7168 into 2 x 2048).  starts[e], shorts[e]: blocks and short blocks before
+// expert e, starts[L], shorts[L]: all of them.
 struct Table {
     int starts[kMaxExperts + 1], first[kMaxExperts], rows[kMaxExperts];
+    uint16_t shorts[kMaxExperts + 2];
 };
 
-// By one wavefront.  Returns whether a window reaches beyond its tensor.
+__host__ __device__ constexpr int short_blocks(int n, int rows) { return n > 0 && n <= rows / 2; }
+__host__ __device__ constexpr int whole_blocks(int n, int rows) { return short_blocks(n, rows) ? 0 : (n + rows - 1) / rows; }
+
+// By one wavefront; SHORTS: short blocks are counted apart.  Returns whether a window reaches beyond its tensor.
+template <bool SHORTS>
 __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, Table* table, int lane) {
-    int* starts = table->starts;
     const int per = (w.L + 63) / 64;
     const int e0 = lane * per, e1 = min(w.L, e0 + per);
-    int sum = 0;
+    int whole = 0, brief = 0;
     bool cut = false;
     for (int e = e0; e < e1; ++e) {
         int64_t at;
@@ -85,25 +92,33 @@ __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, Table* t
         cut |= n < w.count[e];
         table->first[e] = (int)at;
         table->rows[e] = n;
-        sum += (n + rows - 1) / rows;
+        whole += SHORTS ? whole_blocks(n, rows) : (n + rows - 1) / rows;
+        brief += SHORTS ? short_blocks(n, rows) : 0;
     }
-    int before = sum;
+    int w1 = whole, b1 = brief;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(before, d);
-        if (lane >= d) before += v;
+        const int u = __shfl_up(w1, d), v = __shfl_up(b1, d);
+        if (lane >= d) { w1 += u; b1 += v; }
     }
-    int at = before - sum;
+    int wa = w1 - whole, ba = b1 - brief;
     for (int e = e0; e < e1; ++e) {
-        starts[e] = at;
-        at += (table->rows[e] + rows - 1) / rows;
+        table->starts[e] = wa;
+        table->shorts[e] = (uint16_t)ba;
+        const int n = table->rows[e];
+        wa += SHORTS ? whole_blocks(n, rows) : (n + rows - 1) / rows;
+        ba += SHORTS ? short_blocks(n, rows) : 0;
     }
-    if (lane == 63) starts[w.L] = before;
+    if (lane == 63) {
+        table->starts[w.L] = w1;
+        table->shorts[w.L] = (uint16_t)b1;
+    }
     return __any(cut);
 }
 
 // The expert whose blocks hold block b: starts[e] <= b < starts[e + 1].
-__device__ __forceinline__ int find_expert(const int* starts, int L, int b) {
+template <class T>
+__device__ __forceinline__ int find_expert(const T* starts, int L, int b) {
     int lo = 0, hi = L;  // the answer is in [lo, hi)
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -250,23 +265,30 @@ __device__ __forceinline__ void barrier() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-constexpr int kWaves = 8, NWI = 2, NWJ = 4;   // wavefronts of a workgroup, along P and along Q
-constexpr int kBJ = 256;                      // rows per tile
+constexpr int kWaves = 8;            // wavefronts of a workgroup
+constexpr int kBlockRows = 256;      // rows per tile; short blocks: half
 constexpr int kFlatStages = 3;
-// Tiles of 256 along P in two stages, or of 128 in three.
-constexpr int kLdsTiles = std::max(2 * (256 + kBJ) * kBK * 2, kFlatStages * (128 + kBJ) * kBK * 2);
+// Tiles of 256 x 256 in two stages, or half as large ones in three.
+constexpr int kLdsTiles = std::max(2 * (256 + 256) * kBK * 2, kFlatStages * (128 + 256) * kBK * 2);
 
-// Tiles of 256 along P that a row of tiles takes.
-__device__ __forceinline__ int wide_columns(const Product& a, int kind) { return (a.I * (kind == FORWARD && a.gated ? 2 : 1) + 255) / 256; }
+// What the tiles of a launch are: every one 256 along P (I); along Q (J) first the whole blocks, then the short ones.
+struct Tiling {
+    int columns;                // along I
+    int blocks, shorts;         // grad_W: per expert
+    int64_t whole, all;         // tiles of whole blocks, all tiles
+};
 
-// All tiles of one workgroup, BI indices of P by kBJ of Q: tiles [from, from + count) of 256 indices of P, or their halves.
-template <int KIND, int BI>
-__device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table, int64_t from, int64_t count) {
-    constexpr int BJ = kBJ, NW = kWaves;
-    constexpr bool WIDE = BI == 256;
+// Tiles of one workgroup, BI indices of P by BJ of Q:
+//   256 x 256   tiles [t, end) of whole blocks in steps of the grid
+//   256 x 128   tiles [t, end) of short blocks
+//   128 x 256   the halves of the tiles from `from` on, whatever their blocks
+template <int KIND, int BI, int BJ>
+__device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table, const Tiling& tiling, int64_t& t, int64_t from, int64_t end) {
+    constexpr int NW = kWaves, NWI = BJ == 128 ? 4 : 2, NWJ = NW / NWI;   // wavefronts along P and along Q
+    constexpr bool WIDE = BI == 256 && BJ == 256, HALVES = BI == 128;
     constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
     constexpr int WI = BI / NWI, WJ = BJ / NWJ, IT = WI / 16, JT = WJ / 16;
-    constexpr bool kHint = BI == 128 && KIND != GRAD_WEIGHTS;
+    constexpr bool kHint = !WIDE && KIND != GRAD_WEIGHTS;
     using P = Operand<BI, kPK, NW, kHint>;
     using Q = Operand<BJ, kQK, NW, false>;
     constexpr int kStage = P::kBytes + Q::kBytes;
@@ -276,9 +298,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
 
     // A gated tile holds BI/2 outputs: their gate and their up columns.
     const int bi = KIND == FORWARD && a.gated ? BI / 2 : BI;
-    const int ni = wide_columns(a, KIND);
-    const int weight_blocks = KIND == GRAD_WEIGHTS ? (a.J + BJ - 1) / BJ : 0;
-    const int64_t tiles = WIDE ? count : 2 * count;   // first halves, then second halves, of which the last may be empty
+    const int ni = tiling.columns;
 
     // Tile t: expert by expert, within an expert in bands of eight row blocks, within a band column block by column block.
     // Workgroups of one XCD (blockIdx mod 8) take neighbouring tiles, so that its L2 serves both operands.
@@ -288,21 +308,34 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     };
     auto locate = [&](int64_t u) {
         Tile c;
-        const int half = !WIDE && u >= count;
-        const int64_t t = from + (half ? u - count : u);
-        const int block = (int)(t / ni);
-        c.e = __builtin_amdgcn_readfirstlane(KIND == GRAD_WEIGHTS ? block / weight_blocks : find_expert(table->starts, a.win.L, block));
-        const int start = KIND == GRAD_WEIGHTS ? c.e * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[c.e]);
-        const int m = (KIND == GRAD_WEIGHTS ? (c.e + 1) * weight_blocks : __builtin_amdgcn_readfirstlane(table->starts[c.e + 1])) - start;
-        const int64_t local = t - (int64_t)start * ni;
+        const int half = HALVES && u >= end - from;   // first halves, then second halves
+        const int64_t tile = HALVES ? from + (half ? u - (end - from) : u) : u;
+        const bool brief = HALVES ? tile >= tiling.whole : BJ == 128;
+        const int64_t mine = brief ? tile - tiling.whole : tile;
+        const int block = (int)(mine / ni);
+        int start, m, ib;
+        if (KIND == GRAD_WEIGHTS) {
+            m = brief ? tiling.shorts : tiling.blocks;
+            c.e = block / m;
+            start = c.e * m;
+        } else if (brief) {
+            c.e = uniform(find_expert(table->shorts, a.win.L, block));
+            start = block;
+            m = 1;
+        } else {
+            c.e = uniform(find_expert(table->starts, a.win.L, block));
+            start = uniform(table->starts[c.e]);
+            m = uniform(table->starts[c.e + 1]) - start;
+        }
+        const int64_t local = mine - (int64_t)start * ni;
         const int band = (int)(local / (8 * ni)), height = min(8, m - band * 8), in = (int)(local - (int64_t)band * 8 * ni);
-        const int ib = __builtin_amdgcn_readfirstlane(in / height);
-        c.j0 = __builtin_amdgcn_readfirstlane(band * 8 + in - ib * height) * BJ;
-        c.i0 = ib * (WIDE ? bi : 2 * bi) + half * bi;
+        ib = uniform(in / height);
+        c.rows = uniform(table->rows[c.e]);
+        c.first = uniform(table->first[c.e]);
+        c.j0 = uniform(band * 8 + in - ib * height) * kBlockRows;
+        c.i0 = ib * (HALVES ? 2 * bi : bi) + half * bi;
         c.first_i = c.i0 == 0;
-        c.alone = m == 1;
-        c.rows = __builtin_amdgcn_readfirstlane(table->rows[c.e]);
-        c.first = __builtin_amdgcn_readfirstlane(table->first[c.e]);
+        c.alone = KIND != GRAD_WEIGHTS && c.rows <= kBlockRows;
         return c;
     };
     P p;
@@ -352,14 +385,13 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         }
     };
 
-    const int per = gridDim.x >> 3;
-    int64_t t = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    const int64_t tiles = HALVES ? 2 * (end - from) : end;
     Tile c;
     // The workgroup's next tile that is not empty, from t on.
     auto find = [&] {
         for (; t < tiles; t += gridDim.x) {
             c = locate(t);
-            if (WIDE || c.i0 < a.I) return true;
+            if (!HALVES || c.i0 < a.I) return true;   // the second half of a last tile may be empty
         }
         return false;
     };
@@ -666,18 +698,28 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     Table* table = (Table*)(lds + kLdsTiles);
     if (threadIdx.x < 64) {
-        const bool cut = scan_blocks(a.win, kBJ, table, threadIdx.x);
+        const bool cut = scan_blocks<true>(a.win, kBlockRows, table, threadIdx.x);
         if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
     }
     __syncthreads();
-    // Blocks of kBJ rows of the experts that have rows (grad_W: of kBJ weight rows, for every expert), times blocks along I.
-    // They go in rounds of the workgroups.  Where the last round would leave half of them without a tile it takes tiles of 128
-    // along P instead, whose steps take 5/8 of the time: all of them for small inputs, in one round.
-    const int64_t blocks = KIND == GRAD_WEIGHTS ? (int64_t)a.win.L * ((a.J + kBJ - 1) / kBJ) : uniform(table->starts[a.win.L]);
-    const int64_t tiles = blocks * wide_columns(a, KIND), rest = tiles % gridDim.x;
-    const bool halve = 2 * rest <= gridDim.x;
-    product_tiles<KIND, 256>(a, lds, table, 0, halve ? tiles - rest : tiles);
-    if (halve) product_tiles<KIND, 128>(a, lds, table, tiles - rest, rest);
+    // The tiles go in rounds of the workgroups.  Where the last round would leave half of them without a tile it takes halves
+    // instead, whose steps take 5/8 of the time: all of them for small inputs, in one round.
+    Tiling t;
+    t.columns = (a.I * (KIND == FORWARD && a.gated ? 2 : 1) + 255) / 256;
+    t.blocks = KIND == GRAD_WEIGHTS ? whole_blocks(a.J, kBlockRows) : uniform(table->starts[a.win.L]);
+    t.shorts = KIND == GRAD_WEIGHTS ? short_blocks(a.J, kBlockRows) : uniform(table->shorts[a.win.L]);
+    const int64_t experts = KIND == GRAD_WEIGHTS ? a.win.L : 1;
+    t.whole = experts * t.blocks * t.columns;
+    t.all = t.whole + experts * t.shorts * t.columns;
+    int64_t rest = t.all % gridDim.x;
+    if (2 * rest > gridDim.x) rest = 0;
+    const int per = gridDim.x >> 3;
+    const int64_t mine = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    int64_t at = mine;
+    product_tiles<KIND, 256, 256>(a, lds, table, t, at, 0, min(t.whole, t.all - rest));
+    product_tiles<KIND, 256, 128>(a, lds, table, t, at, 0, t.all - rest);
+    at = mine;
+    product_tiles<KIND, 128, 256>(a, lds, table, t, at, t.all - rest, t.all);
 }
 
 // grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows.
@@ -698,7 +740,7 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
 
 __global__ __launch_bounds__(256) void act_backward_kernel(const ActBackwardArgs a) {
     __shared__ Table table;
-    if (threadIdx.x < 64) scan_blocks(a.win, kActRows, &table, threadIdx.x);
+    if (threadIdx.x < 64) scan_blocks<false>(a.win, kActRows, &table, threadIdx.x);
     __syncthreads();
     const int units = a.No / 8;
     for (int b = blockIdx.x; b < table.starts[a.win.L]; b += gridDim.x) {
@@ -770,7 +812,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     p.pre = a.pre.base; p.pre_expert = a.pre.expert_stride; p.pre_row = a.pre.row_stride;
     p.res = a.res.base; p.res_expert = a.res.expert_stride; p.res_row = a.res.row_stride;
     p.status = a.status;
-    return launch<FORWARD>(p, most_blocks(a.win, kBJ), s);
+    return launch<FORWARD>(p, most_blocks(a.win, kBlockRows), s);
 }
 
 hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
@@ -781,7 +823,7 @@ hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
     p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
     p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
     p.I = a.Kd; p.Kc = a.N;
-    return launch<GRAD_ROWS>(p, most_blocks(a.win, kBJ), s);
+    return launch<GRAD_ROWS>(p, most_blocks(a.win, kBlockRows), s);
 }
 
 hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
@@ -793,7 +835,7 @@ hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
     p.out_f32 = a.gw_f32; p.accumulate = a.accumulate;
     p.grad_b = a.grad_b; p.gb_stride = a.gb_stride;
     p.I = a.Kd; p.J = a.N;
-    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + kBJ - 1) / kBJ), s);
+    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + kBlockRows - 1) / kBlockRows), s);
 }
 
 hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s) {
