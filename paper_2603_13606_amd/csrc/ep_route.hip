@@ -74,15 +74,19 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int64_t t = (int64_t)blockIdx.x * kRouteWaves + wave; t < a.T; t += (int64_t)gridDim.x * kRouteWaves) {
         float l[NPL];
-        float top = -__builtin_inff();
 #pragma unroll
         for (int i = 0; i < NPL; ++i) {
             const int e = lane + 64 * i;
             l[i] = e < a.E ? load_logit(a.logits, t * a.logits_stride + e, a.logits_bf16) : -__builtin_inff();
-            top = fmaxf(top, l[i]);
+        }
+        float top = 0.0f;   // the largest logit, where the softmax over all experts is wanted
+        if (a.score == EP_SCORE_SOFTMAX && (SCORES || !a.renormalise)) {
+            top = l[0];
+#pragma unroll
+            for (int i = 1; i < NPL; ++i) top = fmaxf(top, l[i]);
+            top = unordered(wave_max(top > -__builtin_inff() ? ordered(top) : 0u));
         }
         uint32_t hi[NPL], lo[SCORES ? NPL : 1];
-        top = unordered(wave_max(top > -__builtin_inff() ? ordered(top) : 0u));
         if constexpr (!SCORES) {
 #pragma unroll
             for (int i = 0; i < NPL; ++i) hi[i] = l[i] > -__builtin_inff() ? ordered(l[i]) : 0u;
@@ -139,7 +143,9 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
                 worth = __shfl(worth, min(lane, a.groups - 1) * sub);
                 int rank = 0;
                 for (int j = 0; j < a.groups; ++j) {
-                    const double w = __shfl(worth, j);
+                    const uint64_t u = (uint64_t)__double_as_longlong(worth);
+                    const double w = __longlong_as_double((long long)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), j) << 32 |
+                                                                      (uint32_t)__builtin_amdgcn_readlane((int)u, j)));
                     rank += w > worth || (w == worth && j < lane);
                 }
                 const uint64_t kept = __ballot(lane < a.groups && rank < a.kept);
@@ -158,44 +164,82 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
             }
         }
 
+        // Up to four experts per lane are put in order once (neighbours change places, so equal ones stay as they are), and
+        // the lane's best is the first; more are searched in every round.
+        constexpr bool SORTED = NPL <= 4;
+        int at[NPL];   // place j: expert lane + 64 * at[j]
+#pragma unroll
+        for (int i = 0; i < NPL; ++i) at[i] = i;
+        if constexpr (SORTED) {
+#pragma unroll
+            for (int n = NPL - 1; n > 0; --n)
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    const bool swap = SCORES ? hi[i + 1] > hi[i] || (hi[i + 1] == hi[i] && lo[i + 1] > lo[i]) : hi[i + 1] > hi[i];
+                    auto exchange = [swap](auto& x, auto& y) {
+                        const auto z = x;
+                        x = swap ? y : x;
+                        y = swap ? z : y;
+                    };
+                    exchange(hi[i], hi[i + 1]);
+                    if (SCORES) exchange(lo[i], lo[i + 1]);
+                    exchange(at[i], at[i + 1]);
+                }
+        }
         int my_idx = -1;        // lane k: the k-th expert
         float my_l = -__builtin_inff();
         for (int k = 0; k < a.K; ++k) {
-            uint32_t bh = 0, bl = 0, be = 0xffffffffu;
-            float logit = 0.0f;
+            uint32_t bh = hi[0], bl = SCORES ? lo[0] : 0u;
+            int bi = at[0];
+            if constexpr (!SORTED) {
 #pragma unroll
-            for (int i = NPL - 1; i >= 0; --i) {
-                const bool better = SCORES ? hi[i] > bh || (hi[i] == bh && lo[i] >= bl) : hi[i] >= bh;
-                if (better) {
-                    bh = hi[i];
-                    if (SCORES) bl = lo[i];
-                    be = lane + 64 * i;
-                    logit = l[i];
-                }
+                for (int i = 1; i < NPL; ++i)
+                    if (SCORES ? hi[i] > bh || (hi[i] == bh && lo[i] > bl) : hi[i] > bh) {
+                        bh = hi[i];
+                        if (SCORES) bl = lo[i];
+                        bi = i;
+                    }
             }
             const uint32_t mh = wave_max(bh);
             if (mh == 0) break;  // nothing routable is left
             bool mine = bh == mh;
-            if (SCORES) {
-                const uint32_t ml = wave_max(mine ? bl : 0u);
-                mine = mine && bl == ml;
-            }
             uint64_t who = __ballot(mine);
-            if (who & (who - 1)) {  // a tie between lanes: the lowest id
-                const uint32_t e = wave_min(mine ? be : 0xffffffffu);
-                mine = mine && be == e;
+            if (who & (who - 1)) {  // a tie between lanes: the larger low word, then the lowest id
+                if (SCORES) {
+                    const uint32_t ml = wave_max(mine ? bl : 0u);
+                    mine = mine && bl == ml;
+                }
+                const uint32_t e = wave_min(mine ? lane + 64 * bi : 0xffffffffu);
+                mine = mine && lane + 64 * bi == (int)e;
                 who = __ballot(mine);
             }
             const int from = __builtin_ctzll(who);
-            const int e = __builtin_amdgcn_readlane((int)be, from);
-            const float le = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(logit), from));
-            if (lane == k) { my_idx = e; my_l = le; }
+            const int i = __builtin_amdgcn_readlane(bi, from);
+            float logit;
+            if constexpr (SCORES) {
+                logit = l[0];
 #pragma unroll
-            for (int i = 0; i < NPL; ++i)
-                if (mine && (e >> 6) == i) {
-                    hi[i] = 0;
-                    if (SCORES) lo[i] = 0;
+                for (int j = 1; j < NPL; ++j) logit = i == j ? l[j] : logit;
+                logit = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(logit), from));
+            } else {
+                logit = unordered(mh);
+            }
+            if (lane == k) { my_idx = from + 64 * i; my_l = logit; }
+            if constexpr (SORTED) {
+#pragma unroll
+                for (int j = 0; j < NPL; ++j) {
+                    hi[j] = mine ? (j + 1 < NPL ? hi[(j + 1) % NPL] : 0u) : hi[j];
+                    if (SCORES) lo[j] = mine ? (j + 1 < NPL ? lo[(j + 1) % NPL] : 0u) : lo[j];
+                    at[j] = mine && j + 1 < NPL ? at[(j + 1) % NPL] : at[j];
                 }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NPL; ++j)
+                    if (mine && i == j) {
+                        hi[j] = 0;
+                        if (SCORES) lo[j] = 0;
+                    }
+            }
         }
 
         float w;
