@@ -542,7 +542,7 @@ hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
     if (a.gated) split ? up(two(), four()) : up(two(), one());
     else split ? up(one(), four()) : up(one(), one());
     // down: 8 columns per workgroup where 16 would leave compute units without one
-    const bool narrow = (a.H + 15) / 16 < cus;
+    const bool narrow = (a.H + 7) / 8 <= cus;
     const dim3 columns((uint32_t)(narrow ? (a.H + 7) / 8 : (a.H + 15) / 16));
     const size_t lds = (size_t)down_lds(a.T, a.K, plan.slots);
     auto down = [&](auto rows) {
