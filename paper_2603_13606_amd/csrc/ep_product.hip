@@ -28,6 +28,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
+constexpr int kSmall = 64;                    // indices of a small tile along P and along Q
 constexpr int kBK = 64;                       // contraction indices per LDS tile
 constexpr uint32_t kNowhere = 0x80000000u;    // offset of a lane that has nothing there: beyond the buffer's end, reads zeros
 
@@ -70,10 +71,11 @@ __device__ __forceinline__ int window_rows(const Windows& w, int e, int64_t* fir
 // half of that is enough for all of them (the short end of a longer window is a block like the others: it goes next to
 // them, while the weights are in the L2; apart from them it would read the weights again, 668 against 711 us at 32 x 300 rows of
 // 7168 into 2 x 2048).  starts[e], shorts[e]: blocks and short blocks before
-// expert e, starts[L], shorts[L]: all of them.
+// expert e, starts[L], shorts[L]: all of them; smalls: blocks of kSmall rows in all.
 struct Table {
     int starts[kMaxExperts + 1], first[kMaxExperts], rows[kMaxExperts];
     uint16_t shorts[kMaxExperts + 2];
+    int smalls;
 };
 
 __host__ __device__ constexpr int short_blocks(int n, int rows) { return n > 0 && n <= rows / 2; }
@@ -84,7 +86,7 @@ template <bool SHORTS>
 __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, Table* table, int lane) {
     const int per = (w.L + 63) / 64;
     const int e0 = lane * per, e1 = min(w.L, e0 + per);
-    int whole = 0, brief = 0;
+    int whole = 0, brief = 0, small = 0;
     bool cut = false;
     for (int e = e0; e < e1; ++e) {
         int64_t at;
@@ -94,12 +96,13 @@ __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, Table* t
         table->rows[e] = n;
         whole += SHORTS ? whole_blocks(n, rows) : (n + rows - 1) / rows;
         brief += SHORTS ? short_blocks(n, rows) : 0;
+        small += (n + kSmall - 1) / kSmall;
     }
-    int w1 = whole, b1 = brief;
+    int w1 = whole, b1 = brief, s1 = small;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(w1, d), v = __shfl_up(b1, d);
-        if (lane >= d) { w1 += u; b1 += v; }
+        const int u = __shfl_up(w1, d), v = __shfl_up(b1, d), w = __shfl_up(s1, d);
+        if (lane >= d) { w1 += u; b1 += v; s1 += w; }
     }
     int wa = w1 - whole, ba = b1 - brief;
     for (int e = e0; e < e1; ++e) {
@@ -112,8 +115,29 @@ __device__ __forceinline__ bool scan_blocks(const Windows& w, int rows, Table* t
     if (lane == 63) {
         table->starts[w.L] = w1;
         table->shorts[w.L] = (uint16_t)b1;
+        table->smalls = s1;
     }
     return __any(cut);
+}
+
+// The same table in blocks of `rows` rows, none of them apart.  By one wavefront.
+__device__ __forceinline__ void rescan_blocks(int L, int rows, Table* table, int lane) {
+    const int per = (L + 63) / 64;
+    const int e0 = lane * per, e1 = min(L, e0 + per);
+    int all = 0;
+    for (int e = e0; e < e1; ++e) all += (table->rows[e] + rows - 1) / rows;
+    int upto = all;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(upto, d);
+        if (lane >= d) upto += u;
+    }
+    int at = upto - all;
+    for (int e = e0; e < e1; ++e) {
+        table->starts[e] = at;
+        at += (table->rows[e] + rows - 1) / rows;
+    }
+    if (lane == 63) table->starts[L] = upto;
 }
 
 // The expert whose blocks hold block b: starts[e] <= b < starts[e + 1].
@@ -258,6 +282,11 @@ __device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t r, uint32_t off, c
     __builtin_amdgcn_raw_buffer_store_b128(u, r, off, 0, 0);
 }
 
+// Four values of one fragment for one index of Q, as bf16.
+__device__ __forceinline__ void store4(__amdgpu_buffer_rsrc_t r, uint32_t off, const f32x4& v) {
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])}, r, off, 0, 0);
+}
+
 // A barrier that nothing is moved across; it waits for nobody's memory accesses.
 __device__ __forceinline__ void barrier() {
     __builtin_amdgcn_sched_barrier(0);
@@ -268,6 +297,7 @@ __device__ __forceinline__ void barrier() {
 constexpr int kWaves = 8;            // wavefronts of a workgroup
 constexpr int kBlockRows = 256;      // rows per tile; short blocks: half
 constexpr int kFlatStages = 3;
+constexpr int kSmallStages = 4;      // of two steps each
 // Tiles of 256 x 256 in two stages, or half as large ones in three.
 constexpr int kLdsTiles = std::max(2 * (256 + 256) * kBK * 2, kFlatStages * (128 + 256) * kBK * 2);
 
@@ -282,10 +312,12 @@ struct Tiling {
 //   256 x 256   tiles [t, end) of whole blocks in steps of the grid
 //   256 x 128   tiles [t, end) of short blocks
 //   128 x 256   the halves of the tiles from `from` on, whatever their blocks
+//    64 x 64    tiles [t, end) of blocks of 64
 template <int KIND, int BI, int BJ>
 __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table, const Tiling& tiling, int64_t& t, int64_t from, int64_t end) {
     constexpr int NW = kWaves, NWI = BJ == 128 ? 4 : 2, NWJ = NW / NWI;   // wavefronts along P and along Q
-    constexpr bool WIDE = BI == 256 && BJ == 256, HALVES = BI == 128;
+    constexpr bool WIDE = BI == 256 && BJ == 256, HALVES = BI == 128, SMALL = BJ == kSmall;
+    constexpr int kBlock = SMALL ? kSmall : kBlockRows;
     constexpr bool kPK = KIND == FORWARD, kQK = KIND != GRAD_WEIGHTS;
     constexpr int WI = BI / NWI, WJ = BJ / NWJ, IT = WI / 16, JT = WJ / 16;
     constexpr bool kHint = !WIDE && KIND != GRAD_WEIGHTS;
@@ -332,15 +364,25 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         ib = uniform(in / height);
         c.rows = uniform(table->rows[c.e]);
         c.first = uniform(table->first[c.e]);
-        c.j0 = uniform(band * 8 + in - ib * height) * kBlockRows;
+        c.j0 = uniform(band * 8 + in - ib * height) * kBlock;
         c.i0 = ib * (HALVES ? 2 * bi : bi) + half * bi;
         c.first_i = c.i0 == 0;
-        c.alone = KIND != GRAD_WEIGHTS && c.rows <= kBlockRows;
+        c.alone = KIND != GRAD_WEIGHTS && c.rows <= kBlock;
         return c;
     };
     P p;
     Q q;
     auto steps_of = [&](const Tile& c) { return ((KIND == GRAD_WEIGHTS ? c.rows : a.Kc) + kBK - 1) / kBK; };
+    // Small tiles: both steps of a turn.
+    auto load_turn = [&](int stage, int left) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            char* to = lds + (stage * 2 + h) * kStage;
+            p.template load<0, P::kLoads>(to, left - h * kBK, wave);
+            q.template load<0, Q::kLoads>(to + P::kBytes, left - h * kBK, wave);
+            p.next(); q.next();
+        }
+    };
     // Points the operands at a tile and issues its first loads: all of step 0, and of step 1 all (or what its phase 0 reads).
     auto begin = [&](const Tile& c) {
         const int lane = opaque(threadIdx.x & 63);
@@ -363,7 +405,10 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         if constexpr (kQK) q.start_rows(qb + c.j0 * a.q_row, a.q_row, wave, lane, [=](int r) { return r < rows_left ? r : -1; });
         else q.start_cols(qb + c.j0, a.q_row, wave, lane, a.J - c.j0);
         const int Kc = KIND == GRAD_WEIGHTS ? c.rows : a.Kc;
-        if (Kc > 0) {
+        if constexpr (SMALL) {
+#pragma unroll
+            for (int k = 0; k < kSmallStages - 1; ++k) load_turn(k, Kc - k * 2 * kBK);
+        } else if (Kc > 0) {
             p.template load<0, P::kLoads>(lds, Kc, wave);
             q.template load<0, Q::kLoads>(lds + P::kBytes, Kc, wave);
             p.next(); q.next();
@@ -499,6 +544,52 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                 multiply(1);
             }
             if (steps && !late) barrier();
+        } else if constexpr (SMALL) {
+            // Few tiles: what counts is how long one takes.  A turn is two steps of 64 and one barrier, in four stages, so that
+            // the loads of three turns are on their way; behind the last step there are loads too, of nothing, which keeps
+            // their number the same in every turn.  The barrier in front of turn k says that its tiles have landed and that
+            // everybody has read turn k - 1, whose place the loads of turn k + 3 take.
+            int stage = 0;
+            for (int k = 0; k < steps; k += 2) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * (kSmallStages - 2) * kLoads) : "memory");
+                barrier();
+                const char* cur = lds + stage * 2 * kStage;
+                bf16x8 pf[4][IT], qf[4][JT];
+                if (!idle) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const char* pc = cur + h * kStage;
+#pragma unroll
+                        for (int it = 0; it < IT; ++it) {
+                            pf[2 * h][it] = fragment<kPK, 0>(pc, wi * WI + it * 16, pl);
+                            pf[2 * h + 1][it] = fragment<kPK, 1>(pc, wi * WI + it * 16, pl);
+                        }
+#pragma unroll
+                        for (int jt = 0; jt < JT; ++jt) {
+                            qf[2 * h][jt] = fragment<kQK, 0>(pc + P::kBytes, wj * WJ + jt * 16, ql);
+                            qf[2 * h + 1][jt] = fragment<kQK, 1>(pc + P::kBytes, wj * WJ + jt * 16, ql);
+                        }
+                    }
+                }
+                load_turn(stage == 0 ? kSmallStages - 1 : stage - 1, Kc - (k / 2 + kSmallStages - 1) * 2 * kBK);
+                stage = stage == kSmallStages - 1 ? 0 : stage + 1;
+                if (idle) continue;
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+                    for (int it = 0; it < IT; ++it)
+#pragma unroll
+                        for (int jt = 0; jt < JT; ++jt)
+                            acc[it][jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[ks][it], qf[ks][jt], acc[it][jt], 0, 0, 0);
+                    if (with_sums)
+#pragma unroll
+                        for (int jt = 0; jt < JT; ++jt)
+                            sums[jt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, one), qf[ks][jt], sums[jt], 0, 0, 0);
+                }
+            }
+            // everybody's loads, those of nothing too, are done before the next tile's take their places
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            barrier();
         } else {
             // The same two groups with one load interval (all fragments of a step, 64 KiB of LDS reads per group) and one
             // product interval (32 instructions, as long) per step, and three stages: the loads of step k + 2 take the place
@@ -602,23 +693,25 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             if (a.pre) {
                 const auto rp = buffer(a.pre + done.e * a.pre_expert + (done.first + done.j0) * a.pre_row + done.i0);
 #pragma unroll
-                for (int it = 0; it < IT; it += 2)
+                for (int it = 0; it < IT; it += SMALL ? 1 : 2)
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
-                        const int i = i8 + (it < nit ? it : it - nit) * 16;
-                        store8(rp, at(jt, i, a.pre_row, 2) + (it < nit || i >= Il ? 0 : a.I * 2), acc[it][jt], acc[it + 1][jt]);
+                        const int i = (SMALL ? i4 : i8) + (it < nit ? it : it - nit) * 16;
+                        const uint32_t to = at(jt, i, a.pre_row, 2) + (it < nit || i >= Il ? 0 : a.I * 2);
+                        if constexpr (SMALL) store4(rp, to, acc[it][jt]);
+                        else store8(rp, to, acc[it][jt], acc[it + 1][jt]);
                     }
             }
             const auto rr = buffer(a.res + done.e * a.res_expert + (done.first + done.j0) * a.res_row + done.i0);
             auto finish = [&](auto activation, auto gate) {
-                constexpr int kN = decltype(gate)::value ? IT / 2 : IT;
+                constexpr int kN = decltype(gate)::value ? IT / 2 : IT, kH = SMALL ? 1 : 2;
 #pragma unroll
-                for (int it = 0; it < kN; it += 2)
+                for (int it = 0; it < kN; it += kH)
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
-                        f32x4 v[2];
+                        f32x4 v[kH];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                        for (int h = 0; h < kH; ++h) {
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 v[h][r] = activate(decltype(activation)::value, acc[it + h][jt][r]);
@@ -630,7 +723,8 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                                 for (int r = 0; r < 4; ++r) v[h][r] += res[r];
                             }
                         }
-                        store8(ro, at(jt, i8 + it * 16, a.out_row, 2), v[0], v[1]);
+                        if constexpr (SMALL) store4(ro, at(jt, i4 + it * 16, a.out_row, 2), v[0]);
+                        else store8(ro, at(jt, i8 + it * 16, a.out_row, 2), v[0], v[1]);
                     }
             };
             auto with = [&](auto activation) {
@@ -711,14 +805,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a
     const int64_t experts = KIND == GRAD_WEIGHTS ? a.win.L : 1;
     t.whole = experts * t.blocks * t.columns;
     t.all = t.whole + experts * t.shorts * t.columns;
+    const int per = gridDim.x >> 3;
+    // The place of this workgroup in a round of n tiles, as many on each XCD and neighbours together; n where it has none.
+    auto place = [&](int64_t n) {
+        const int each = (int)(n + 7) >> 3, in = blockIdx.x >> 3;
+        return in < each ? (int64_t)(blockIdx.x & 7) * each + in : n;
+    };
+    Tiling small = {(a.I * (KIND == FORWARD && a.gated ? 2 : 1) + kSmall - 1) / kSmall,
+                    KIND == GRAD_WEIGHTS ? (a.J + kSmall - 1) / kSmall : uniform(table->smalls), 0, 0, 0};
+    small.all = experts * small.blocks * small.columns;
+    if (small.all <= gridDim.x) {
+        if (KIND != GRAD_WEIGHTS) {
+            if (threadIdx.x < 64) rescan_blocks(a.win.L, kSmall, table, threadIdx.x);
+            __syncthreads();
+        }
+        int64_t at = place(small.all);
+        product_tiles<KIND, kSmall, kSmall>(a, lds, table, small, at, 0, small.all);
+        return;
+    }
     int64_t rest = t.all % gridDim.x;
     if (2 * rest > gridDim.x) rest = 0;
-    const int per = gridDim.x >> 3;
     const int64_t mine = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
     int64_t at = mine;
     product_tiles<KIND, 256, 256>(a, lds, table, t, at, 0, min(t.whole, t.all - rest));
     product_tiles<KIND, 256, 128>(a, lds, table, t, at, 0, t.all - rest);
-    at = mine;
+    at = place(2 * rest);
     product_tiles<KIND, 128, 256>(a, lds, table, t, at, t.all - rest, t.all);
 }
 
@@ -778,7 +889,7 @@ template <int KIND>
 hipError_t launch(const Product& a, int64_t most_row_blocks, hipStream_t s) {
     constexpr int lds = kLdsTiles + (int)sizeof(Table);
     static_assert(lds <= 160 * 1024, "a compute unit's LDS");
-    const int bi = KIND == FORWARD && a.gated ? 64 : 128;   // of the narrow tiles
+    const int bi = KIND == FORWARD && a.gated ? kSmall / 2 : kSmall;
     const int64_t most = most_row_blocks * ((a.I + bi - 1) / bi);
     if (most <= 0) return hipSuccess;
     const int64_t cus = std::max(8, compute_units() / 8 * 8);
@@ -812,7 +923,7 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     p.pre = a.pre.base; p.pre_expert = a.pre.expert_stride; p.pre_row = a.pre.row_stride;
     p.res = a.res.base; p.res_expert = a.res.expert_stride; p.res_row = a.res.row_stride;
     p.status = a.status;
-    return launch<FORWARD>(p, most_blocks(a.win, kBlockRows), s);
+    return launch<FORWARD>(p, most_blocks(a.win, kSmall), s);
 }
 
 hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
@@ -823,7 +934,7 @@ hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
     p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
     p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
     p.I = a.Kd; p.Kc = a.N;
-    return launch<GRAD_ROWS>(p, most_blocks(a.win, kBlockRows), s);
+    return launch<GRAD_ROWS>(p, most_blocks(a.win, kSmall), s);
 }
 
 hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
@@ -835,7 +946,7 @@ hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
     p.out_f32 = a.gw_f32; p.accumulate = a.accumulate;
     p.grad_b = a.grad_b; p.gb_stride = a.gb_stride;
     p.I = a.Kd; p.J = a.N;
-    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + kBlockRows - 1) / kBlockRows), s);
+    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + kSmall - 1) / kSmall), s);
 }
 
 hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s) {
