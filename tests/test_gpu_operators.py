@@ -283,6 +283,67 @@ def test_expert_product_backward(ep, counts, Kd, No, activation, gated, padded):
     assert torch.equal(gw2, gw)
 
 
+def cycle(counts, n):
+    return [counts[i % len(counts)] for i in range(n)]
+
+
+# Enough tiles for every compute unit: tall windows, short ones, both, last rounds that are part full; 1 to 25 contraction steps.
+MANY = [
+    (cycle([140, 129, 250, 256, 257, 130, 200], 70), 264, 264), (cycle([1, 128, 0, 17, 64, 65, 100], 140), 72, 136),
+    (cycle([1, 128, 0, 17, 64, 65, 100], 140), 72, 120), (cycle([10, 200, 128, 129, 0, 300, 64], 140), 320, 200),
+    (cycle([150, 131], 140), 40, 16), (cycle([160, 3], 90), 128, 264), (cycle([130, 20, 280], 40), 1600, 1000),
+    (cycle([600, 90, 0], 12), 200, 2056), (cycle([3, 8], 1024), 64, 48),
+]
+
+
+@pytest.mark.parametrize("counts,Kd,No", MANY)
+@pytest.mark.parametrize("activation,gated,options", [("none", False, "bias residual"), ("silu", True, "bias pre"), ("gelu", False, "residual pre"),
+                                                      ("gelu", True, "bias residual pre")])
+def test_expert_product_with_many_tiles(ep, counts, Kd, No, activation, gated, options):
+    c = Case(counts, Kd, No, gated, padded=activation == "silu", seed=2)
+    x = c.tokens(Kd)
+    bias = normal(c.gen, c.L, c.N, dtype=torch.bfloat16 if gated else torch.float32) if "bias" in options else None
+    res = c.tokens(No) if "residual" in options else None
+    pre = c.fresh(c.N) if "pre" in options else None
+    out = c.fresh(No)
+    ep.ep_expert_product(x, c.w, out, bias=bias, residual=res, pre=pre, row_offset=c.offset, row_count=c.count,
+                         activation=getattr(ep, "EP_ACT_" + activation.upper()), gated=gated)
+    flat, fres = x.reshape(c.rows, Kd), res.reshape(c.rows, No) if res is not None else None
+    want = [ref.product(flat[f:f + n], c.w[e], bias[e] if bias is not None else None, fres[f:f + n] if res is not None else None, activation, gated)
+            for e, (f, n) in enumerate(zip(c.first, c.counts))]
+    c.check(out, lambda e, s: want[e][:2], "out")
+    if pre is not None:
+        c.check(pre, lambda e, s: want[e][2:], "pre")
+
+
+@pytest.mark.parametrize("counts,Kd,No", MANY)
+@pytest.mark.parametrize("activation,gated,wide,accumulate", [("none", False, True, True), ("silu", True, False, False), ("gelu", False, True, False),
+                                                              ("gelu", True, False, True)])
+def test_expert_product_backward_with_many_tiles(ep, counts, Kd, No, activation, gated, wide, accumulate):
+    c = Case(counts, Kd, No, gated, padded=activation == "silu", seed=3)
+    x, g = c.tokens(Kd), c.tokens(No)
+    pre = c.tokens(c.N) if activation != "none" or gated else None
+    gp, gx = c.fresh(c.N) if pre is not None else None, c.fresh(Kd)
+    t = torch.float32 if wide else torch.bfloat16
+    start_w, start_b = normal(c.gen, c.L, c.N, Kd, dtype=t), normal(c.gen, c.L, c.N, dtype=t)
+    gw, gb = start_w.clone(), start_b.clone()
+    ep.ep_expert_product_backward(g, c.w, x=x, pre=pre, grad_pre=gp, grad_x=gx, grad_weights=gw, grad_bias=gb, row_offset=c.offset,
+                                  row_count=c.count, activation=getattr(ep, "EP_ACT_" + activation.upper()), gated=gated, accumulate=accumulate)
+    flat = lambda t: t.reshape(c.rows, -1)  # noqa: E731
+    want = [ref.product_grad(flat(g)[f:f + n], c.w[e], flat(x)[f:f + n], flat(pre)[f:f + n] if pre is not None else None, activation, gated)
+            for e, (f, n) in enumerate(zip(c.first, c.counts))]
+    if pre is not None:
+        c.check(gp, lambda e, s: want[e]["grad_pre"], "grad_pre")
+    c.check(gx, lambda e, s: want[e]["grad_x"], "grad_x")
+    for got, start, name in ((gw, start_w, "grad_w"), (gb, start_b, "grad_b")):
+        for e in range(c.L):
+            v, b = want[e][name]
+            if accumulate:
+                v = v + start[e].double()
+                b = b + ref.U32 * v.abs()
+            within(got[e], v, b + (0 if wide else ref.BF16 * (v.abs() + b)), f"{name} of expert {e}")
+
+
 def test_expert_product_windows_beyond_the_tensors_are_cut(ep):
     """Offsets and counts that do not fit: negative, beyond the end, across it."""
     gen = gen_of(9)
