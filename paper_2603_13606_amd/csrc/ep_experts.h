@@ -102,8 +102,8 @@ struct GradWeightsArgs {
 
 hipError_t launch_product(const ProductArgs& a, hipStream_t s);
 hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s);
-hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s);
-hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s);
+// Either may be nullptr; both have the same windows and grad_pre.
+hipError_t launch_gradients(const GradRowsArgs* rows, const GradWeightsArgs* weights, hipStream_t s);
 
 // ---- the layer of few tokens ------------------------------------------------------------------
 

@@ -248,7 +248,6 @@ ep_result_t ep_expert_product_backward(ep_handle_t handle, const ep_product_conf
         rows.win = r.win; rows.grad_pre = grad_pre; rows.grad_x = gxd;
         rows.w = (const uint16_t*)w->data; rows.w_expert = w->stride[0]; rows.w_row = w->stride[1];
         rows.N = (int)N; rows.Kd = (int)Kd;
-        if (launch_grad_rows(rows, (hipStream_t)stream) != hipSuccess) return EP_ERR_HIP;
     }
     if (gw) {
         weights.win = r.win; weights.grad_pre = grad_pre; weights.x = xd;
@@ -256,9 +255,8 @@ ep_result_t ep_expert_product_backward(ep_handle_t handle, const ep_product_conf
         weights.gw_f32 = gw->dtype == EP_DTYPE_F32;
         weights.grad_b = gb ? gb->data : nullptr; weights.gb_stride = gb ? gb->stride[0] : 0;
         weights.N = (int)N; weights.Kd = (int)Kd; weights.accumulate = cfg->accumulate;
-        if (launch_grad_weights(weights, (hipStream_t)stream) != hipSuccess) return EP_ERR_HIP;
     }
-    return EP_SUCCESS;
+    return gx || gw ? done(launch_gradients(gx ? &rows : nullptr, gw ? &weights : nullptr, (hipStream_t)stream)) : EP_SUCCESS;
 }
 
 ep_result_t ep_expert_layer_plan(int64_t num_tokens, int32_t top_k, int32_t num_experts, int32_t hidden, int32_t inner,

@@ -822,17 +822,13 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     }
 }
 
+// All tiles of a product, by the workgroups of the grid, as the table has them.  `in`: the workgroup's place among those of
+// its XCD.  Returns how many of each XCD had a tile of the last pass (0: any).
 template <int KIND>
-__global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a) {
-    extern __shared__ __attribute__((aligned(1024))) char lds[];
-    Table* table = (Table*)(lds + kLdsTiles);
-    if (threadIdx.x < 64) {
-        const bool cut = scan_blocks<true>(a.win, kBlockRows, table, threadIdx.x);
-        if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
-    }
-    __syncthreads();
+__device__ __forceinline__ int product(const Product& a, char* lds, Table* table, int in) {
     // The tiles go in rounds of the workgroups.  Where the last round would leave half of them without a tile it takes halves
-    // instead, whose steps take 5/8 of the time: all of them for small inputs, in one round.
+    // instead, whose steps take 5/8 of the time: all of them for small inputs, in one round.  Where even tiles of 64 x 64
+    // fit one round, those.
     Tiling t;
     t.columns = (a.I * (KIND == FORWARD && a.gated ? 2 : 1) + 255) / 256;
     t.blocks = KIND == GRAD_WEIGHTS ? whole_blocks(a.J, kBlockRows) : uniform(table->starts[a.win.L]);
@@ -843,7 +839,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a
     const int per = gridDim.x >> 3;
     // The place of this workgroup in a round of n tiles, as many on each XCD and neighbours together; n where it has none.
     auto place = [&](int64_t n) {
-        const int each = (int)(n + 7) >> 3, in = blockIdx.x >> 3;
+        const int each = (int)(n + 7) >> 3;
         return in < each ? (int64_t)(blockIdx.x & 7) * each + in : n;
     };
     Tiling small = {(a.I * (KIND == FORWARD && a.gated ? 2 : 1) + kSmall - 1) / kSmall,
@@ -856,16 +852,40 @@ __global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a
         }
         int64_t at = place(small.all);
         product_tiles<KIND, kSmall, kSmall>(a, lds, table, small, at, 0, small.all);
-        return;
+        return (int)(small.all + 7) >> 3;
     }
     int64_t rest = t.all % gridDim.x;
     if (2 * rest > gridDim.x) rest = 0;
-    const int64_t mine = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    const int64_t mine = (int64_t)(blockIdx.x & 7) * per + in;
     int64_t at = mine;
     product_tiles<KIND, 256, 256>(a, lds, table, t, at, 0, min(t.whole, t.all - rest));
     product_tiles<KIND, 256, 128>(a, lds, table, t, at, 0, t.all - rest);
     at = place(2 * rest);
     product_tiles<KIND, 128, 256>(a, lds, table, t, at, t.all - rest, t.all);
+    return (int)(2 * rest + 7) >> 3;
+}
+
+template <int KIND>
+__global__ __launch_bounds__(64 * kWaves, 2) void product_kernel(const Product a) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    Table* table = (Table*)(lds + kLdsTiles);
+    if (threadIdx.x < 64) {
+        const bool cut = scan_blocks<true>(a.win, kBlockRows, table, threadIdx.x);
+        if (KIND == FORWARD && cut && a.status && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.status, STATUS_OUTPUT_OVERFLOW);
+    }
+    __syncthreads();
+    product<KIND>(a, lds, table, blockIdx.x >> 3);
+}
+
+// Both gradients in one launch: where the tiles of grad_x do not fill the last round, those of grad_W begin.
+__global__ __launch_bounds__(64 * kWaves, 2) void gradients_kernel(const Product x, const Product w) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    Table* table = (Table*)(lds + kLdsTiles);
+    if (threadIdx.x < 64) scan_blocks<true>(x.win, kBlockRows, table, threadIdx.x);
+    __syncthreads();
+    const int per = gridDim.x >> 3, in = blockIdx.x >> 3;
+    const int used = product<GRAD_ROWS>(x, lds, table, in) % per;
+    product<GRAD_WEIGHTS>(w, lds, table, in >= used ? in - used : in - used + per);
 }
 
 // grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows.
@@ -920,18 +940,27 @@ int64_t most_blocks(const Windows& w, int rows) {
     return w.cap / rows + w.L;
 }
 
-template <int KIND>
-hipError_t launch(const Product& a, int64_t most_row_blocks, hipStream_t s) {
-    constexpr int lds = kLdsTiles + (int)sizeof(Table);
-    static_assert(lds <= 160 * 1024, "a compute unit's LDS");
-    const int bi = KIND == FORWARD && a.gated ? kSmall / 2 : kSmall;
-    const int64_t most = most_row_blocks * ((a.I + bi - 1) / bi);
-    if (most <= 0) return hipSuccess;
+// Tiles of a product that there can be at most, small ones.
+int64_t most_tiles(const Windows& w, int columns, int per_expert) {
+    return (per_expert ? (int64_t)w.L * per_expert : most_blocks(w, kSmall)) * columns;
+}
+
+uint32_t product_grid(int64_t most) {
     const int64_t cus = std::max(8, compute_units() / 8 * 8);
-    const int64_t grid = std::min(cus, (most + 7) / 8 * 8);
-    hipLaunchKernelGGL(product_kernel<KIND>, dim3((uint32_t)grid), dim3(64 * kWaves), lds, s, a);
+    return (uint32_t)std::min(cus, (most + 7) / 8 * 8);
+}
+
+constexpr int kLds = kLdsTiles + (int)sizeof(Table);
+static_assert(kLds <= 160 * 1024, "a compute unit's LDS");
+
+template <int KIND>
+hipError_t launch(const Product& a, int64_t most, hipStream_t s) {
+    if (most <= 0) return hipSuccess;
+    hipLaunchKernelGGL(product_kernel<KIND>, dim3(product_grid(most)), dim3(64 * kWaves), kLds, s, a);
     return hipGetLastError();
 }
+
+int small_blocks(int n) { return (n + kSmall - 1) / kSmall; }
 
 }  // namespace
 
@@ -958,30 +987,38 @@ hipError_t launch_product(const ProductArgs& a, hipStream_t s) {
     p.pre = a.pre.base; p.pre_expert = a.pre.expert_stride; p.pre_row = a.pre.row_stride;
     p.res = a.res.base; p.res_expert = a.res.expert_stride; p.res_row = a.res.row_stride;
     p.status = a.status;
-    return launch<FORWARD>(p, most_blocks(a.win, kSmall), s);
+    return launch<FORWARD>(p, most_tiles(a.win, small_blocks(a.gated ? 2 * a.No : a.No), 0), s);
 }
 
-hipError_t launch_grad_rows(const GradRowsArgs& a, hipStream_t s) {
-    Product p = {};
-    p.win = a.win;
-    p.p = a.w; p.p_expert = a.w_expert; p.p_row = a.w_row;
-    p.p_lines = (uintptr_t)a.w % 128 == 0 && a.w_expert % 64 == 0 && a.w_row % 64 == 0;
-    p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
-    p.out = a.grad_x.base; p.out_expert = a.grad_x.expert_stride; p.out_row = a.grad_x.row_stride;
-    p.I = a.Kd; p.Kc = a.N;
-    return launch<GRAD_ROWS>(p, most_blocks(a.win, kSmall), s);
-}
-
-hipError_t launch_grad_weights(const GradWeightsArgs& a, hipStream_t s) {
-    Product p = {};
-    p.win = a.win;
-    p.p = a.x.base; p.p_expert = a.x.expert_stride; p.p_row = a.x.row_stride;
-    p.q = a.grad_pre.base; p.q_expert = a.grad_pre.expert_stride; p.q_row = a.grad_pre.row_stride;
-    p.out = (uint16_t*)a.grad_w; p.out_expert = a.gw_expert; p.out_row = a.gw_row;
-    p.out_f32 = a.gw_f32; p.accumulate = a.accumulate;
-    p.grad_b = a.grad_b; p.gb_stride = a.gb_stride;
-    p.I = a.Kd; p.J = a.N;
-    return launch<GRAD_WEIGHTS>(p, (int64_t)a.win.L * ((a.N + kSmall - 1) / kSmall), s);
+hipError_t launch_gradients(const GradRowsArgs* rows, const GradWeightsArgs* weights, hipStream_t s) {
+    Product x = {}, w = {};
+    int64_t most_x = 0, most_w = 0;
+    if (rows) {
+        const GradRowsArgs& a = *rows;
+        x.win = a.win;
+        x.p = a.w; x.p_expert = a.w_expert; x.p_row = a.w_row;
+        x.p_lines = (uintptr_t)a.w % 128 == 0 && a.w_expert % 64 == 0 && a.w_row % 64 == 0;
+        x.q = a.grad_pre.base; x.q_expert = a.grad_pre.expert_stride; x.q_row = a.grad_pre.row_stride;
+        x.out = a.grad_x.base; x.out_expert = a.grad_x.expert_stride; x.out_row = a.grad_x.row_stride;
+        x.I = a.Kd; x.Kc = a.N;
+        most_x = most_tiles(a.win, small_blocks(a.Kd), 0);
+    }
+    if (weights) {
+        const GradWeightsArgs& a = *weights;
+        w.win = a.win;
+        w.p = a.x.base; w.p_expert = a.x.expert_stride; w.p_row = a.x.row_stride;
+        w.q = a.grad_pre.base; w.q_expert = a.grad_pre.expert_stride; w.q_row = a.grad_pre.row_stride;
+        w.out = (uint16_t*)a.grad_w; w.out_expert = a.gw_expert; w.out_row = a.gw_row;
+        w.out_f32 = a.gw_f32; w.accumulate = a.accumulate;
+        w.grad_b = a.grad_b; w.gb_stride = a.gb_stride;
+        w.I = a.Kd; w.J = a.N;
+        most_w = most_tiles(a.win, small_blocks(a.Kd), small_blocks(a.N));
+    }
+    if (!weights) return launch<GRAD_ROWS>(x, most_x, s);
+    if (!rows) return launch<GRAD_WEIGHTS>(w, most_w, s);
+    if (most_x + most_w <= 0) return hipSuccess;
+    hipLaunchKernelGGL(gradients_kernel, dim3(product_grid(most_x + most_w)), dim3(64 * kWaves), kLds, s, x, w);
+    return hipGetLastError();
 }
 
 hipError_t launch_act_backward(const ActBackwardArgs& a, hipStream_t s) {
