@@ -133,7 +133,9 @@ struct LayerArgs {
 struct LayerPlan {
     int64_t mid, total;          // the sorted entries come first, then the rows between the products
     int slots;                   // experts that can be named: min(L, T * K)
-    int up_parts;                // workgroups per named expert in the first launch
+    int up_parts;                // shares of a named expert's rows in the first launch, a workgroup each
+    int token_parts;             // shares of its tokens, too
+    int token_step;              // tokens per pass over the weights
 };
 void plan_layer(int T, int K, int L, int H, int inner, LayerPlan* p);
 hipError_t launch_layer(const LayerArgs& a, hipStream_t s);

@@ -291,7 +291,8 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
         sort_entries(a, plan, ids, (int*)(ids + kLayerMaxTokens * kMaxTopK));
         return;
     }
-    const int slot = (blockIdx.x - 1) / plan.up_parts, part = (blockIdx.x - 1) % plan.up_parts;
+    const int unit = (blockIdx.x - 1) / plan.token_parts, token_part = (blockIdx.x - 1) % plan.token_parts;
+    const int slot = unit / plan.up_parts, part = unit % plan.up_parts;
 
     // the slot-th of the experts that any token names
     const uint32_t word = lane < kMaxExperts / 32 ? named[lane] : 0u;
@@ -379,20 +380,21 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
         weight_offsets(wo, a.up_row, a.inner - i0, lane);
         __amdgpu_buffer_rsrc_t w[G];
         weights_of(i0, w);
-        for (int p0 = 0; p0 < n; p0 += kGroups * 16) {
+        for (int p0 = token_part * plan.token_step; p0 < n; p0 += plan.token_parts * plan.token_step) {
+            const int p1 = min(n, p0 + plan.token_step);
             uint32_t xo[kGroups];
             f32x4 acc[G][kGroups];
 #pragma unroll
             for (int jt = 0; jt < kGroups; ++jt) {
                 const int pos = p0 + jt * 16 + (lane & 15);
-                xo[jt] = pos < n ? (uint32_t)(s_token[pos] * a.x_stride * 2) : kNowhere;
+                xo[jt] = pos < p1 ? (uint32_t)(s_token[pos] * a.x_stride * 2) : kNowhere;
 #pragma unroll
                 for (int g = 0; g < G; ++g) acc[g][jt] = f32x4{0, 0, 0, 0};
             }
-            multiply_groups<G, kUpDepth, kRows, NT>(n - p0, acc, w, wo, x, xo, rings[wave], wave % SPLIT, blocks, SPLIT, a.H, lane);
+            multiply_groups<G, kUpDepth, kRows, NT>(p1 - p0, acc, w, wo, x, xo, rings[wave], wave % SPLIT, blocks, SPLIT, a.H, lane);
 #pragma unroll
             for (int jt = 0; jt < kGroups; ++jt) {
-                if (p0 + jt * 16 >= n) break;
+                if (p0 + jt * 16 >= p1) break;
                 f32x4 sum[G];
 #pragma unroll
                 for (int g = 0; g < G; ++g) sum[g] = acc[g][jt];
@@ -514,7 +516,7 @@ void plan_layer(int T, int K, int L, int H, int inner, LayerPlan* p) {
     p->slots = (int)std::min<int64_t>(L, (int64_t)T * K);
     p->mid = up256(sorted_words(p->slots, T * K) * 4);
     p->total = p->mid + up256((int64_t)T * K * inner * 2);
-    p->up_parts = 0;
+    p->up_parts = p->token_parts = p->token_step = 0;
 }
 
 hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
@@ -530,7 +532,12 @@ hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
     const bool split = (int64_t)plan.slots * slices < 2 * kUpWaves * (int64_t)cus;
     const int runs = split ? slices : (slices + kUpWaves - 1) / kUpWaves;
     plan.up_parts = std::clamp((4 * cus + plan.slots - 1) / plan.slots, 1, runs);
-    const dim3 grid((uint32_t)(plan.slots * plan.up_parts + 1)), block(64 * kUpWaves);
+    // Where that leaves compute units idle, the tokens of an expert are shared out too: its weights then come from the L2.
+    const int groups = (a.T + 15) / 16;
+    const int shares = split ? std::clamp(2 * cus / (plan.slots * plan.up_parts), 1, groups) : 1;
+    plan.token_step = 16 * std::min(kGroups, (groups + shares - 1) / shares);
+    plan.token_parts = std::min(shares, (a.T + plan.token_step - 1) / plan.token_step);
+    const dim3 grid((uint32_t)(plan.slots * plan.up_parts * plan.token_parts + 1)), block(64 * kUpWaves);
     auto up = [&](auto g, auto n) {
         constexpr int G = decltype(g)::value, S = decltype(n)::value;
         if (lines(a.w_up, a.up_expert, a.up_row) && (!a.gated || a.inner * a.up_row % 64 == 0)) hipLaunchKernelGGL((layer_up_kernel<G, S, true>), grid, block, 0, s, a, plan);

@@ -417,6 +417,15 @@ LAYERS = [
     (5, 64, 70, 40, 24, "silu", True, {}),
     (7, 3, 5, 64, 32, "silu", True, dict(masked=1.0, residual=True)),  # nobody is routed here
     (7, 3, 5, 64, 32, "silu", True, dict(masked=1.0)),
+    # enough runs of rows for every wavefront; more output columns than compute units can take by eights; whole lines or not
+    (64, 8, 64, 128, 1040, "silu", True, dict(bias=torch.bfloat16)),
+    (128, 8, 64, 72, 1088, "gelu", False, dict(residual=True)),
+    (128, 4, 8, 128, 8256, "silu", True, {}),
+    (9, 2, 4, 2368, 64, "silu", True, dict(residual=True)),
+    (9, 2, 4, 2312, 72, "gelu", False, dict(bias=torch.float32)),
+    (70, 1, 1, 2304, 128, "silu", True, {}),
+    (128, 2, 1, 2120, 200, "silu", False, dict(first=1)),
+    (50, 2, 4, 4168, 136, "silu", True, {}),
 ]
 
 
