@@ -291,7 +291,10 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
         sort_entries(a, plan, ids, (int*)(ids + kLayerMaxTokens * kMaxTopK));
         return;
     }
-    const int unit = (blockIdx.x - 1) / plan.token_parts, token_part = (blockIdx.x - 1) % plan.token_parts;
+    // the shares of an expert's tokens on the same XCD, whose L2 they have the weights from
+    const int units = plan.slots * plan.up_parts, pitch8 = (units + 7) & ~7;
+    const int unit = (blockIdx.x - 1) % pitch8, token_part = (blockIdx.x - 1) / pitch8;
+    if (unit >= units) return;
     const int slot = unit / plan.up_parts, part = unit % plan.up_parts;
 
     // the slot-th of the experts that any token names
@@ -537,7 +540,7 @@ hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
     const int shares = split ? std::clamp(2 * cus / (plan.slots * plan.up_parts), 1, groups) : 1;
     plan.token_step = 16 * std::min(kGroups, (groups + shares - 1) / shares);
     plan.token_parts = std::min(shares, (a.T + plan.token_step - 1) / plan.token_step);
-    const dim3 grid((uint32_t)(plan.slots * plan.up_parts * plan.token_parts + 1)), block(64 * kUpWaves);
+    const dim3 grid((uint32_t)((plan.slots * plan.up_parts + 7) / 8 * 8 * plan.token_parts + 1)), block(64 * kUpWaves);
     auto up = [&](auto g, auto n) {
         constexpr int G = decltype(g)::value, S = decltype(n)::value;
         if (lines(a.w_up, a.up_expert, a.up_row) && (!a.gated || a.inner * a.up_row % 64 == 0)) hipLaunchKernelGGL((layer_up_kernel<G, S, true>), grid, block, 0, s, a, plan);
