@@ -138,7 +138,8 @@ def test_empty_calls_launch_nothing(ep):
 
 def test_layer_plan(ep):
     p = ep.ep_expert_layer_plan(128, 8, 256, 7168, 2048)
-    assert p.slots == 256 and p.workspace_bytes >= 128 * 8 * 2048 * 2 + 256 * (2 + 2 * 128) * 4
+    # the rows between the products, one per entry; the entries by expert: a count, ids, starts and one more, the entries
+    assert p.slots == 256 and p.workspace_bytes >= 128 * 8 * 2048 * 2 + (1 + 256 + 256 + 1 + 128 * 8) * 4
     assert ep.ep_expert_layer_plan(3, 2, 256, 64, 16).slots == 6
     for bad in ((129, 8, 8, 64, 16), (-1, 8, 8, 64, 16), (1, 0, 8, 64, 16), (1, 65, 8, 64, 16), (1, 1, 0, 64, 16), (1, 1, 1025, 64, 16),
                 (1, 1, 8, 60, 16), (1, 1, 8, 64, 12), (1, 1, 8, 64, 1 << 18)):
