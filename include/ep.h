@@ -610,7 +610,7 @@ typedef struct {
  * ep_route -- the gate: the K experts of each token and their weights, as ep_layout, ep_dispatch and
  * ep_combine take them.
  * inputs:  LOGITS l [T, E] f32 or bf16, any row stride (E <= 1024); SELECT_BIAS b f32 [E] (optional).
- * outputs: TOPK_IDX int32 [T, K] (K <= 64); TOPK_WEIGHTS f32 [T, K].
+ * outputs: TOPK_IDX int32 [T, K] (K <= 64, T * K <= 2^28); TOPK_WEIGHTS f32 [T, K].
  * s = softmax(l) over the token's routable experts, or sigmoid(l).  An expert is not routable where its
  * logit is -inf or NaN (or its bias is); +inf counts as the largest finite float.  The K routable experts
  * with the largest s + b are taken in descending order, ties to the lower id; with groups only experts of
@@ -653,7 +653,8 @@ typedef struct {
  * handle:  the routing whose windows the row tensors are (concatenated [rows, .] or padded
  *          [num_experts, C, .], strides as for ep_dispatch); weights of L experts from first_expert on.  Or NULL, and the
  *          windows come with the call: ROW_COUNT int32 [L] rows of each expert and, for 2-D row tensors,
- *          ROW_OFFSET int32 [L] its first row; 3-D row tensors [L, C, .] have theirs at [e, 0 .. count).
+ *          ROW_OFFSET int32 [L] its first row; 3-D row tensors [L, C, .] have theirs at [e, 0 .. count).  A row
+ *          lies in one window at most.
  * inputs:  TOKENS x, rows of Kd bf16; EXPERT_WEIGHTS W bf16 [L, N, Kd]; EXPERT_BIAS b f32 or bf16 [L, N]
  *          (optional); RESIDUAL r, rows like the output (optional).
  * outputs: TOKENS out, rows of N (gated: N/2) bf16; PREACT, rows of N bf16 (optional): what
@@ -662,7 +663,8 @@ typedef struct {
  * with float32 accumulation and one rounding to bf16 (of pre as delivered, and of out).  Rows outside the
  * windows are left untouched.  Rows of a window beyond the shortest row tensor are skipped and, with a
  * handle, flagged (status bit 2).  r may be out itself.
- * N (and N/2), Kd multiples of 8; every row on a 16-byte boundary, rows less than 2^22 elements apart;
+ * N (and N/2), Kd multiples of 8; every row on a 16-byte boundary, rows less than 2^22 elements apart, the
+ * rows of an output apart from each other;
  * a gated expert's weights span less than 2^31 bytes (else EP_ERR_UNSUPPORTED).  One expert is a plain
  * matrix product with bias, activation and residual.
  * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED, EP_ERR_HIP.
@@ -711,8 +713,9 @@ EP_API ep_result_t ep_expert_layer_plan(int64_t num_tokens, int32_t top_k, int32
  * e = idx[t,k] - first_expert; ids outside [first_expert, first_expert + L) (-1, other ranks' experts)
  * contribute nothing.  An expert may be named twice by a token.  w * act(.) is rounded to bf16 between the
  * two products; sums are float32 in a fixed order.  H and I multiples of 8, at most 2^17; rows on
- * 16-byte boundaries, less than 2^22 elements apart.
- * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED (more than 128 tokens), EP_ERR_HIP.
+ * 16-byte boundaries, less than 2^22 elements apart.  It is made for up to 16 tokens per expert; with many
+ * more (few experts, many tokens) dispatch, two products and combine are faster.
+ * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED (more than 128 tokens, or T * K * I >= 2^30), EP_ERR_HIP.
  */
 EP_API ep_result_t ep_expert_layer(const ep_product_config_t *cfg, const ep_tensor_t *inputs, int32_t num_inputs,
                                    const ep_tensor_t *outputs, int32_t num_outputs, ep_stream_t stream);

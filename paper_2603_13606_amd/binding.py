@@ -593,7 +593,7 @@ class PreparedOperator:
 
     def __init__(self, fn_name: str, cfg, ins, outs, takes_handle: bool = False):
         ins, outs = [p for p in ins if p[0] is not None], [p for p in outs if p[0] is not None]
-        _one_device([t for t, _ in ins + outs])
+        self._device = _one_device([t for t, _ in ins + outs])
         self._fn = getattr(load(), fn_name)
         self._name = fn_name
         self._cfg = cfg
@@ -602,6 +602,8 @@ class PreparedOperator:
         self._args = (ctypes.byref(cfg), _descs(ins), len(ins), _descs(outs), len(outs))
 
     def __call__(self, handle=None, stream_ptr: int = 0) -> None:
+        if self._device is not None and torch.cuda.current_device() != self._device:
+            raise ValueError(f"prepared for cuda:{self._device}, current device cuda:{torch.cuda.current_device()}")
         code = self._fn(handle, *self._args, stream_ptr) if self._takes_handle else self._fn(*self._args, stream_ptr)
         if code != EP_SUCCESS:
             raise EpError(code, self._name)
@@ -611,11 +613,12 @@ class PreparedOperator:
         self(handle, _stream_ptr(stream))
 
 
-def _one_device(tensors) -> None:
-    """The library launches on the current device: a tensor of another one is the caller's mistake."""
+def _one_device(tensors) -> Optional[int]:
+    """The library launches on the current device: a tensor of another one is the caller's mistake.  Returns the device."""
     gpu = {t.device for t in tensors if t.is_cuda}
     if len(gpu) > 1 or (gpu and next(iter(gpu)).index != torch.cuda.current_device()):
         raise ValueError(f"tensors on {sorted(map(str, gpu))}, current device cuda:{torch.cuda.current_device()}")
+    return next(iter(gpu)).index if gpu else None
 
 
 def _route_config(score, renormalise, num_groups, groups_kept, scale) -> ep_route_config_t:

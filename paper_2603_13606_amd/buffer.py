@@ -288,6 +288,8 @@ class EPBuffer:
         """grad_x, grad_pre = expert_product_backward(grad_out, handle, weights, x, pre): the gradient of the rows (given the
         weights; zeros outside the windows) and of the pre-activation; gradients of weights and bias go to the tensors given
         for them (bf16 or float32), or are added to what they hold."""
+        if weights is None and grad_weights is None:
+            raise ValueError("nothing to compute: neither weights nor grad_weights")
         shape = (weights if weights is not None else grad_weights).shape
         grad_pre = torch.empty_like(pre) if pre is not None else None
         grad_x = torch.zeros((*grad_out.shape[:-1], shape[2]), dtype=torch.bfloat16, device=grad_out.device) if weights is not None else None
@@ -412,7 +414,7 @@ class EPRouteFn(torch.autograd.Function):
 
 class EPExpertProductFn(torch.autograd.Function):
     """Forward: the experts' product on a handle's windows.  Backward: the gradients of rows, weights, bias and residual
-    with the same handle."""
+    with the same handle.  The rows' gradient is 0 outside the windows; the residual's is that of the output as it came."""
 
     @staticmethod
     def forward(ctx, x, weights, bias, residual, buf: EPBuffer, handle: EPHandle, activation="none", gated=False):

@@ -13,6 +13,7 @@ namespace {
 
 constexpr int64_t kMaxExtent = 1 << 22;      // rows' lengths and strides, elements: a tile's offsets stay below 2^31 bytes
 constexpr int64_t kMaxLayerExtent = 1 << 17; // of the layer: its grid stays below 2^32 work-items
+constexpr int64_t kMaxLayerRows = 1 << 30;   // elements between the layer's products: 32-bit byte offsets
 constexpr int kMaxGroups = 64;
 
 bool float_or_bf16(const ep_tensor_t* t) { return t->dtype == EP_DTYPE_F32 || t->dtype == EP_DTYPE_BF16; }
@@ -43,6 +44,13 @@ ep_result_t check_product_config(const ep_product_config_t* c) {
     if (c->activation < EP_ACT_NONE || c->activation > EP_ACT_GELU) return EP_ERR_INVALID_ARG;
     if ((c->gated != 0 && c->gated != 1) || (c->accumulate != 0 && c->accumulate != 1) || c->first_expert < 0) return EP_ERR_INVALID_ARG;
     return EP_SUCCESS;
+}
+
+// Whether no two rows of a 3-D tensor share elements: what is written has to be.
+bool apart(const ep_tensor_t* t) {
+    const int64_t a = t->shape[0], b = t->shape[1], k = t->shape[2], sa = t->stride[0], sb = t->stride[1];
+    if (a <= 1 || b < 1) return true;
+    return sa >= (b - 1) * sb + k || (sa >= k && sb >= (a - 1) * sa + k);
 }
 
 // bf16 (or f32 where allowed) [L, n, k] with rows on 16-byte boundaries.
@@ -105,7 +113,7 @@ ep_result_t find_windows(ep_handle_t h, const ep_product_config_t* cfg, const ep
 }
 
 // A tensor of bf16 rows of `cols` elements in the windows of the call; the shortest tensor bounds the rows.
-bool row_tensor(const ep_tensor_t* t, int64_t cols, Rows* r, RowsDesc* d) {
+bool row_tensor(const ep_tensor_t* t, int64_t cols, Rows* r, RowsDesc* d, bool written = false) {
     if (!t || t->dtype != EP_DTYPE_BF16 || !aligned16(t->data)) return false;
     const int inner = r->padded ? 2 : 1;
     if (t->ndim != inner + 1 || t->shape[inner] != cols || t->stride[inner] != 1) return false;
@@ -114,7 +122,7 @@ bool row_tensor(const ep_tensor_t* t, int64_t cols, Rows* r, RowsDesc* d) {
     if (r->padded) {
         if (t->shape[0] != r->tensor_experts || t->shape[1] != r->slots || t->shape[1] < 0 || t->shape[1] > 0x7fffffffLL) return false;
         if (t->stride[0] < 0 || t->stride[0] % 8) return false;
-        if (!t->data && t->shape[1] > 0) return false;
+        if ((!t->data && t->shape[1] > 0) || (written && !apart(t))) return false;
         d->expert_stride = t->stride[0];
         d->base = (uint16_t*)t->data + r->first * t->stride[0];
     } else {
@@ -192,7 +200,7 @@ ep_result_t ep_expert_product(ep_handle_t handle, const ep_product_config_t* cfg
     Rows r;
     if (ep_result_t e = find_windows(handle, cfg, inputs, num_inputs, L, x, &r); e != EP_SUCCESS) return e;
     ProductArgs a = {};
-    if (!row_tensor(x, Kd, &r, &a.x) || !row_tensor(out, No, &r, &a.out) || (pre && !row_tensor(pre, N, &r, &a.pre)) ||
+    if (!row_tensor(x, Kd, &r, &a.x) || !row_tensor(out, No, &r, &a.out, true) || (pre && !row_tensor(pre, N, &r, &a.pre, true)) ||
         (res && !row_tensor(res, No, &r, &a.res)))
         return EP_ERR_INVALID_ARG;
     a.win = r.win; a.status = r.status;
@@ -218,7 +226,7 @@ ep_result_t ep_expert_product_backward(ep_handle_t handle, const ep_product_conf
     const bool elementwise = cfg->activation != EP_ACT_NONE || cfg->gated;
     if ((gx && !w) || (!w && !gw) || (gw && !x) || (gb && !gw)) return EP_ERR_INVALID_ARG;
     if (elementwise != (pre != nullptr) || elementwise != (gp != nullptr)) return EP_ERR_INVALID_ARG;
-    if ((w && !check_weights(w)) || (gw && !check_weights(gw, true))) return EP_ERR_INVALID_ARG;
+    if ((w && !check_weights(w)) || (gw && !(check_weights(gw, true) && apart(gw)))) return EP_ERR_INVALID_ARG;
     if (w && gw)
         for (int i = 0; i < 3; ++i)
             if (w->shape[i] != gw->shape[i]) return EP_ERR_INVALID_ARG;
@@ -235,10 +243,10 @@ ep_result_t ep_expert_product_backward(ep_handle_t handle, const ep_product_conf
     if (!row_tensor(go, No, &r, &act.grad_out)) return EP_ERR_INVALID_ARG;
     RowsDesc grad_pre = act.grad_out;
     if (elementwise) {
-        if (!row_tensor(pre, N, &r, &act.pre) || !row_tensor(gp, N, &r, &act.grad_pre)) return EP_ERR_INVALID_ARG;
+        if (!row_tensor(pre, N, &r, &act.pre) || !row_tensor(gp, N, &r, &act.grad_pre, true)) return EP_ERR_INVALID_ARG;
         grad_pre = act.grad_pre;
     }
-    if ((gw && !row_tensor(x, Kd, &r, &xd)) || (gx && !row_tensor(gx, Kd, &r, &gxd))) return EP_ERR_INVALID_ARG;
+    if ((gw && !row_tensor(x, Kd, &r, &xd)) || (gx && !row_tensor(gx, Kd, &r, &gxd, true))) return EP_ERR_INVALID_ARG;
     if (handle) handle_used(handle, (hipStream_t)stream);
     if (elementwise) {
         act.win = r.win; act.N = (int)N; act.No = (int)No; act.act = cfg->activation; act.gated = cfg->gated;
@@ -265,6 +273,7 @@ ep_result_t ep_expert_layer_plan(int64_t num_tokens, int32_t top_k, int32_t num_
         num_experts > kMaxExperts || hidden < 8 || hidden % 8 || hidden > kMaxLayerExtent || inner < 8 || inner % 8 ||
         inner > kMaxLayerExtent)
         return EP_ERR_INVALID_ARG;
+    if (num_tokens * top_k * inner >= kMaxLayerRows) return EP_ERR_UNSUPPORTED;
     LayerPlan p;
     plan_layer((int)num_tokens, top_k, num_experts, hidden, inner, &p);
     plan->workspace_bytes = p.total;
@@ -291,6 +300,7 @@ ep_result_t ep_expert_layer(const ep_product_config_t* cfg, const ep_tensor_t* i
     const int64_t T = x->shape[0], K = idx->shape[1], L = up->shape[0], H = up->shape[2], N = up->shape[1], I = cfg->gated ? N / 2 : N;
     if (T > kLayerMaxTokens) return EP_ERR_UNSUPPORTED;
     if (T < 0 || K < 1 || K > kMaxTopK || I % 8 || H > kMaxLayerExtent || I > kMaxLayerExtent) return EP_ERR_INVALID_ARG;
+    if (T * K * I >= kMaxLayerRows) return EP_ERR_UNSUPPORTED;
     if (down->shape[0] != L || down->shape[1] != H || down->shape[2] != I) return EP_ERR_INVALID_ARG;
     auto token_rows = [&](const ep_tensor_t* t) {
         return check_2d(t, EP_DTYPE_BF16, T, H, true) && t->stride[0] % 8 == 0 && t->stride[0] < kMaxExtent && aligned16(t->data);

@@ -33,14 +33,15 @@ constexpr int kGroups = 4;    // groups of 16 tokens per pass over the weights
 constexpr uint32_t kNowhere = 0x80000000u;  // offset of a lane that has nothing to load: reads zeros
 
 // The routed entries by expert, as the second launch wants them (in the workspace): the number of named experts, their
-// ids and where their entries start (one more than there are experts), then the entries, token << 16 | row of the
-// workspace.  A token that names an expert twice has one entry.
+// ids and where their entries start (one more than there are experts), then the entries: t * K + k, which is the row between
+// the products.  A token that names an expert twice has one entry.  All of them are below 2^16: 128 tokens of 64 entries.
 struct Sorted {
-    int32_t *count, *expert, *start, *entry;
+    uint16_t *count, *expert, *start, *entry;
 };
-__host__ __device__ constexpr int64_t sorted_words(int slots, int entries) { return 1 + slots + slots + 1 + entries; }
+static_assert(kLayerMaxTokens * kMaxTopK < 1 << 16 && kMaxExperts < 1 << 16, "16 bits");
+__host__ __device__ constexpr int64_t sorted_words(int slots, int entries) { return (2 + 2 * slots + entries + 1) / 2; }   // of 32 bits
 __host__ __device__ inline Sorted sorted_at(uint8_t* base, int slots) {
-    int32_t* p = (int32_t*)base;
+    uint16_t* p = (uint16_t*)base;
     return {p, p + 1, p + 1 + slots, p + 2 + 2 * slots};
 }
 
@@ -249,21 +250,21 @@ __device__ __forceinline__ void sort_entries(const LayerArgs& a, const LayerPlan
         for (int i = 0; i < kPer; ++i) {
             fill[e0 + i] = at;
             if (n[i] > 0) {
-                out.expert[slot] = e0 + i;
-                out.start[slot] = at;
+                out.expert[slot] = (uint16_t)(e0 + i);
+                out.start[slot] = (uint16_t)at;
                 ++slot;
                 at += n[i];
             }
         }
         if (lane == 63) {
-            *out.count = n1;
-            out.start[n1] = s1;
+            *out.count = (uint16_t)n1;
+            out.start[n1] = (uint16_t)s1;
         }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < a.T * a.K; i += 64 * kUpWaves) {
         const int e = entry_id(i);
-        if (e >= 0) out.entry[atomicAdd(&fill[e], 1)] = (i / a.K) << 16 | i;
+        if (e >= 0) out.entry[atomicAdd(&fill[e], 1)] = (uint16_t)i;
     }
 }
 
@@ -429,11 +430,12 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     float* sums = (float*)(lds + kDownWaves * kDownDepth * kWeightBlock);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h0 = blockIdx.x * ROWS;
-    int32_t* words = (int32_t*)(sums + kDownWaves * a.T * 16);
-    for (int i = threadIdx.x; i < (int)sorted_words(plan.slots, a.T * a.K); i += 64 * kDownWaves) words[i] = ((const int32_t*)a.workspace)[i];
+    uint32_t* words = (uint32_t*)(sums + kDownWaves * a.T * 16);
+    for (int i = threadIdx.x; i < (int)sorted_words(plan.slots, a.T * a.K); i += 64 * kDownWaves) words[i] = ((const uint32_t*)a.workspace)[i];
     for (int i = threadIdx.x; i < kDownWaves * a.T * 16; i += 64 * kDownWaves) sums[i] = 0.0f;
     __syncthreads();
     const Sorted table = sorted_at((uint8_t*)words, plan.slots);
+    auto token_of = [&](uint32_t entry) { return entry / (uint32_t)a.K; };
     float* mine = sums + wave * a.T * 16;
 
     const auto x = buffer(a.workspace + plan.mid);
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     uint32_t wo[2];
     weight_offsets(wo, a.down_row, min(ROWS, a.H - h0), lane);
     int most = 0;   // entries of one expert
-    for (int i = lane; i < *table.count; i += 64) most = max(most, table.start[i + 1] - table.start[i]);
+    for (int i = lane; i < *table.count; i += 64) most = max(most, (int)table.start[i + 1] - (int)table.start[i]);
     if (!__any(most > 16)) {
         stream<1, kDownDepth, ROWS, NT>(q, end, blocks, x, ring, a.inner, lane,
             [&](int slot, __amdgpu_buffer_rsrc_t (&w)[1], uint32_t (&to)[2], uint32_t& row) {
@@ -453,12 +455,12 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
                 to[1] = wo[1];
                 const int e = __builtin_amdgcn_readfirstlane(table.expert[slot]), pos = table.start[slot] + (lane & 15);
                 w[0] = buffer(a.w_down + e * a.down_expert + (int64_t)h0 * a.down_row);
-                row = pos < table.start[slot + 1] ? (uint32_t)(table.entry[pos] & 0xffff) * (uint32_t)a.inner * 2 : kNowhere;
+                row = pos < table.start[slot + 1] ? (uint32_t)table.entry[pos] * (uint32_t)a.inner * 2 : kNowhere;
             },
             [&](int slot, const f32x4 (&acc)[1]) {
                 const int pos = table.start[slot] + (lane & 15);
                 if (pos < table.start[slot + 1] && (lane >> 4) * 4 < ROWS) {
-                    f32x4* to = (f32x4*)(mine + (table.entry[pos] >> 16) * 16 + (lane >> 4) * 4);
+                    f32x4* to = (f32x4*)(mine + token_of(table.entry[pos]) * 16 + (lane >> 4) * 4);
                     *to = *to + acc[0];
                 }
             });
@@ -476,7 +478,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
 #pragma unroll
             for (int jt = 0; jt < kGroups; ++jt) {
                 const int pos = p0 + jt * 16 + (lane & 15);
-                xo[jt] = pos < n ? (uint32_t)(table.entry[first + pos] & 0xffff) * (uint32_t)a.inner * 2 : kNowhere;
+                xo[jt] = pos < n ? (uint32_t)table.entry[first + pos] * (uint32_t)a.inner * 2 : kNowhere;
                 acc[0][jt] = f32x4{0, 0, 0, 0};
             }
             multiply_groups<1, kDownDepth, ROWS, NT>(n - p0, acc, w, wo, x, xo, ring, b0, b1, 1, a.inner, lane);
@@ -484,7 +486,7 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
             for (int jt = 0; jt < kGroups; ++jt) {
                 const int pos = p0 + jt * 16 + (lane & 15);
                 if (pos < n && (lane >> 4) * 4 < ROWS) {
-                    f32x4* to = (f32x4*)(mine + (table.entry[first + pos] >> 16) * 16 + (lane >> 4) * 4);
+                    f32x4* to = (f32x4*)(mine + token_of(table.entry[first + pos]) * 16 + (lane >> 4) * 4);
                     *to = *to + acc[0][jt];
                 }
             }

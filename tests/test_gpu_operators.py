@@ -360,6 +360,41 @@ def test_expert_product_windows_beyond_the_tensors_are_cut(ep):
     assert (gw[2:] == 0).all() and torch.isfinite(gw).all()
 
 
+def test_expert_product_interleaved_windows(ep):
+    """Padded windows that lie between each other: [C, L, .] seen as [L, C, .]."""
+    gen = gen_of(17)
+    counts, C, Kd, No = [5, 0, 9, 70], 70, 136, 72
+    L, cnt = len(counts), torch.tensor([5, 0, 9, 70], dtype=torch.int32, device=DEV)
+    x, w = normal(gen, C, L, Kd).transpose(0, 1), normal(gen, L, No, Kd, std=0.1)
+    out = torch.full((C, L, No), POISON, dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    ep.ep_expert_product(x, w, out, row_count=cnt)
+    gx = torch.full((C, L, Kd), POISON, dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    gw = torch.empty((No, L, Kd), dtype=torch.bfloat16, device=DEV).transpose(0, 1)
+    g = normal(gen, L, C, No)
+    ep.ep_expert_product_backward(g, w, x=x, grad_x=gx, grad_weights=gw, row_count=cnt)
+    for e, n in enumerate(counts):
+        assert out[e, n:].isnan().all() and gx[e, n:].isnan().all()
+        want = ref.product_grad(g[e, :n], w[e], x[e, :n])
+        within(gw[e], want["grad_w"][0], want["grad_w"][1] + ref.BF16 * (want["grad_w"][0].abs() + want["grad_w"][1]), "grad_w")
+        if n:
+            within(out[e, :n], *ref.product(x[e, :n], w[e])[:2], "out")
+            within(gx[e, :n], *want["grad_x"], "grad_x")
+
+
+def test_no_rows_at_all(ep):
+    """Windows without rows: nothing is written but the zeros of the weights' gradients."""
+    w, cnt = torch.randn((3, 24, 64), device=DEV).bfloat16(), torch.zeros(3, dtype=torch.int32, device=DEV)
+    out = torch.full((3, 5, 24), POISON, dtype=torch.bfloat16, device=DEV)
+    x, gw, gb = torch.full((3, 5, 64), POISON, dtype=torch.bfloat16, device=DEV), torch.full((3, 24, 64), POISON, device=DEV), torch.full((3, 24), POISON, device=DEV)
+    ep.ep_expert_product(x, w, out, row_count=cnt)
+    gx = x.clone()
+    ep.ep_expert_product_backward(out, w, x=x, grad_x=gx, grad_weights=gw, grad_bias=gb, row_count=cnt)
+    assert out.isnan().all() and gx.isnan().all() and (gw == 0).all() and (gb == 0).all()
+    gw.fill_(POISON)
+    ep.ep_expert_product_backward(out[:, :0], x=x[:, :0], grad_weights=gw, row_count=cnt)
+    assert (gw == 0).all()
+
+
 def test_expert_product_special_values(ep):
     """A row's NaN or infinity stays in its row; an expert's in its expert."""
     gen = gen_of(11)
@@ -425,6 +460,7 @@ LAYERS = [
     (9, 2, 4, 2312, 72, "gelu", False, dict(bias=torch.float32)),
     (70, 1, 1, 2304, 128, "silu", True, {}),
     (128, 2, 1, 2120, 200, "silu", False, dict(first=1)),
+    (128, 64, 1024, 48, 16, "silu", True, dict(masked=0.1)),          # as many entries as there can be
     (50, 2, 4, 4168, 136, "silu", True, {}),
 ]
 

@@ -79,6 +79,19 @@ def test_expert_product_refuses(ep, change, code):
             row_offset=a["offset"], row_count=a["count"], **kw)
 
 
+def test_outputs_whose_rows_share_memory_are_refused(ep):
+    """Expanded outputs, or windows that reach into each other; interleaved ones are fine (empty here: nothing is launched)."""
+    x, cnt = bf(3, 5, 64), i32(3)
+    for out in (bf(1, 5, 24).expand(3, 5, 24), bf(216).as_strided((3, 5, 24), (48, 24, 1))):
+        refused(ep, ep.EP_ERR_INVALID_ARG, ep.ep_expert_product, x, bf(3, 24, 64), out, row_count=cnt)
+        refused(ep, ep.EP_ERR_INVALID_ARG, ep.ep_expert_product, x, bf(3, 24, 64), bf(3, 5, 24), pre=out, row_count=cnt)
+        refused(ep, ep.EP_ERR_INVALID_ARG, ep.ep_expert_product_backward, x, bf(3, 64, 24), grad_x=out, row_count=cnt)
+    for gw in (bf(1, 24, 64).expand(3, 24, 64), bf(24, 64).as_strided((3, 16, 64), (64, 64, 1))):
+        refused(ep, ep.EP_ERR_INVALID_ARG, ep.ep_expert_product_backward, bf(3, 5, gw.shape[1]), x=x, grad_weights=gw, row_count=cnt)
+    none = bf(3, 0, 64)
+    ep.ep_expert_product(none, bf(3, 24, 64), bf(0, 3, 24).transpose(0, 1), row_count=cnt, stream=0)
+
+
 def test_expert_product_refuses_far_rows(ep):
     """Rows 2^22 elements apart, and a gated expert whose weights span 2^31 bytes."""
     d = ep.tensor_desc(bf(10, 64), ep.EP_TAG_TOKENS)
@@ -139,10 +152,10 @@ def test_empty_calls_launch_nothing(ep):
 def test_layer_plan(ep):
     p = ep.ep_expert_layer_plan(128, 8, 256, 7168, 2048)
     # the rows between the products, one per entry; the entries by expert: a count, ids, starts and one more, the entries
-    assert p.slots == 256 and p.workspace_bytes >= 128 * 8 * 2048 * 2 + (1 + 256 + 256 + 1 + 128 * 8) * 4
+    assert p.slots == 256 and p.workspace_bytes >= 128 * 8 * 2048 * 2 + (1 + 256 + 256 + 1 + 128 * 8) * 2
     assert ep.ep_expert_layer_plan(3, 2, 256, 64, 16).slots == 6
     for bad in ((129, 8, 8, 64, 16), (-1, 8, 8, 64, 16), (1, 0, 8, 64, 16), (1, 65, 8, 64, 16), (1, 1, 0, 64, 16), (1, 1, 1025, 64, 16),
-                (1, 1, 8, 60, 16), (1, 1, 8, 64, 12), (1, 1, 8, 64, 1 << 18)):
+                (1, 1, 8, 60, 16), (1, 1, 8, 64, 12), (1, 1, 8, 64, 1 << 18), (128, 64, 8, 64, 1 << 17)):
         with pytest.raises(ep.EpError):
             ep.ep_expert_layer_plan(*bad)
 
