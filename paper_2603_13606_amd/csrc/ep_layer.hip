@@ -78,8 +78,7 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 // and in the second eight weight rows, its unit included; xo: its token's row in each group, kNowhere if there is none.
 template <int G, int JT, int DEPTH, int ROWS, bool NT>
 __device__ __forceinline__ void multiply(f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
-                                         __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride, int K,
-                                         int lane) {
+                                         __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride, int K, int lane) {
     constexpr int kHalves = ROWS / 8, kLoads = kHalves * G + 2 * JT;   // per block
     bf16x8 xf[DEPTH][JT][2];
     const int wk = ((lane & 7) ^ (lane >> 3)) * 8, xk = (lane >> 4) * 8;
@@ -164,10 +163,11 @@ __device__ __forceinline__ void stream(int64_t q0, int64_t q1, int blocks, __amd
     for (int g = 0; g < G; ++g) acc[g] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d) load(d);
+    // Whole rounds, the last one filled up with loads and products of nothing: a way out in between would join the way back to
+    // the top, and the compiler would then wait there for all loads in every round.
     for (int left = (int)(q1 - q0); left > 0;) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
-            if (left <= 0) break;
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 1) * kLoads) : "memory");
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -181,7 +181,7 @@ __device__ __forceinline__ void stream(int64_t q0, int64_t q1, int blocks, __amd
             __builtin_amdgcn_sched_barrier(0);
             load(d);
             --left;
-            if (++b == blocks || left == 0) {
+            if (left >= 0 && (++b == blocks || left == 0)) {
                 close(run, acc);
 #pragma unroll
                 for (int g = 0; g < G; ++g) acc[g] = f32x4{0, 0, 0, 0};
@@ -193,11 +193,124 @@ __device__ __forceinline__ void stream(int64_t q0, int64_t q1, int blocks, __amd
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing writes to the ring any more
 }
 
+// The same where the rows of weights do not start on lines.  Loaded as they are wanted, each line would come in two parts, at
+// two times (20 tokens of 64 experts, 3512 and 2 x 1208: 396 us; by lines 299).  So the lines themselves are loaded, each once: chunk c of a row is its
+// c-th line, and a block of 64 indices lies in chunks b and b + 1, from unit `shift` of the row on.  Items [q0, q1) as
+// above; weights(run, g) points at the first of a run's rows, of which rows(run) exist, `stride` elements apart; row(run) is the
+// lane's token row.
+template <int G, int DEPTH, int ROWS, class Weights, class Rows, class Row, class Close>
+__device__ __forceinline__ void stream_lines(int64_t q0, int64_t q1, int blocks, int64_t stride, __amdgpu_buffer_rsrc_t x, char* ring, int K, int lane,
+                                             Weights weights, Rows rows, Row row, Close close) {
+    constexpr int kHalves = ROWS / 8, kLoads = kHalves * G + 2;
+    if (q0 >= q1) return;
+    const int unit = (lane & 7) ^ (lane >> 3), xk = (lane >> 4) * 8;
+    struct Place {          // a chunk: those of a run's part [from, to) are from, .., to
+        int run, chunk, from, to, rest;   // rest: blocks of later runs
+    };
+    auto first = [&](int run, int from, int rest) {
+        const int to = min(blocks, from + rest);
+        return Place{run, from, from, to, rest - (to - from)};
+    };
+    Place in = first((int)(q0 / blocks), (int)(q0 % blocks), (int)(q1 - q0)), out = in;   // to load next, to multiply next
+    __amdgpu_buffer_rsrc_t w[G];
+    uint32_t wo[G][kHalves], xo;
+    int shift[G][kHalves];          // units before the row's first in its first line
+    auto open = [&] {
+        const int there = rows(in.run);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const uintptr_t p = (uintptr_t)weights(in.run, g);
+            const uint32_t phase = (uint32_t)p & 127;
+            w[g] = buffer((const void*)(p - phase));
+#pragma unroll
+            for (int s = 0; s < kHalves; ++s) {
+                const int r = s * 8 + (lane >> 3);
+                const uint32_t off = (uint32_t)(r * stride * 2) + phase;
+                wo[g][s] = r < there ? (off & ~127u) + unit * 16 : kNowhere;
+                shift[g][s] = (off & 127) >> 4;
+            }
+        }
+        xo = row(in.run);
+    };
+    uint32_t at[G][2];   // the lane's unit of a fragment in its chunk, and whether that is the second one
+    bool next[G][2];
+    auto aim = [&] {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const int r = lane & 15;
+            const uint32_t off = (uint32_t)(r * stride * 2) + ((uint32_t)(uintptr_t)weights(out.run, g) & 127);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int u = s * 4 + (lane >> 4) + (int)((off & 127) >> 4);
+                at[g][s] = g * kWeightBlock + r * 128 + (((u & 7) ^ (r & 7)) << 4);
+                next[g][s] = u > 7;
+            }
+        }
+    };
+    bf16x8 xf[DEPTH][2];
+    int to_load = (int)(q1 - q0) + (int)((q1 - 1) / blocks - q0 / blocks) + 1;
+    auto load = [&](int d) {
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int s = 0; s < kHalves; ++s) {
+                const bool there = to_load > 0 && (uint32_t)(in.chunk * 8 + unit - shift[g][s]) < (uint32_t)K / 8;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(w[g], (lds_ptr)(ring + (d * G + g) * kWeightBlock + s * 1024), 16,
+                                                         (wo[g][s] + in.chunk * 128) | (there ? 0 : kNowhere), 0, 0, kNonTemporal);
+            }
+        const int block = in.chunk - 1, left = to_load > 0 && in.chunk > in.from ? K - block * kBlock : 0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            xf[d][s] = load8(x, (xo + (uint32_t)(block * kBlock + s * 32 + xk) * 2) | (s * 32 + xk < left ? 0 : kNowhere));
+        --to_load;
+        if (in.chunk++ == in.to && to_load > 0) {
+            in = first(in.run + 1, 0, in.rest);
+            open();
+        }
+    };
+    f32x4 acc[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) acc[g] = f32x4{0, 0, 0, 0};
+    int left = to_load;
+    open();
+    aim();
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d) load(d);
+    while (left > 0) {   // whole rounds, as above
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            constexpr int kSlot = G * kWeightBlock;
+            const int before = (d + DEPTH - 1) % DEPTH;
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 2) * kLoads) : "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            if (left > 0 && out.chunk > out.from) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        const bf16x8 wf = *(const bf16x8*)(ring + at[g][s] + (next[g][s] ? d : before) * kSlot);
+                        acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[d][s], acc[g], 0, 0, 0);
+                    }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // both chunks have been read before the earlier one's place is loaded again
+            __builtin_amdgcn_sched_barrier(0);
+            load(before);
+            if (--left >= 0 && out.chunk++ == out.to) {
+                close(out.run, acc);
+#pragma unroll
+                for (int g = 0; g < G; ++g) acc[g] = f32x4{0, 0, 0, 0};
+                out = first(out.run + 1, 0, out.rest);
+                if (left > 0) aim();
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // nothing writes to the ring any more
+}
+
 // By the number of tokens: the more groups, the fewer blocks of them fit the registers.
 template <int G, int DEPTH, int ROWS, bool NT>
 __device__ __forceinline__ void multiply_groups(int n, f32x4 (&acc)[G][kGroups], const __amdgpu_buffer_rsrc_t (&w)[G], const uint32_t (&wo)[2],
-                                                __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride,
-                                                int K, int lane) {
+                                                __amdgpu_buffer_rsrc_t x, const uint32_t (&xo)[kGroups], char* ring, int b0, int b1, int stride, int K, int lane) {
     if (n <= 16) multiply<G, 1, DEPTH, ROWS, NT>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
     else if (n <= 32) multiply<G, 2, 3, ROWS, NT>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
     else multiply<G, 4, 2, ROWS, NT>(acc, w, wo, x, xo, ring, b0, b1, stride, K, lane);
@@ -364,17 +477,23 @@ __global__ __launch_bounds__(64 * kUpWaves, 2) void layer_up_kernel(const LayerA
     };
     constexpr int kRuns = kUpWaves / SPLIT;   // of rows, next to each other
     const int first = part * kRuns + wave / SPLIT, pitch = plan.up_parts * kRuns;
+    auto slice_weights = [&](int slice, int g) { return a.w_up + e * a.up_expert + (int64_t)(slice * kRows + g * a.inner) * a.up_row; };
     if (SPLIT == 1 && n <= 16) {
         const int mine = first < slices ? (slices - first + pitch - 1) / pitch : 0;
         const uint32_t xo = (lane & 15) < n ? (uint32_t)(s_token[lane & 15] * a.x_stride * 2) : kNowhere;
-        stream<G, kUpDepth, kRows, NT>(0, (int64_t)mine * blocks, blocks, x, rings[wave], a.H, lane,
-            [&](int run, __amdgpu_buffer_rsrc_t (&w)[G], uint32_t (&wo)[2], uint32_t& row) {
-                const int i0 = (first + run * pitch) * kRows;
-                weights_of(i0, w);
-                weight_offsets(wo, a.up_row, a.inner - i0, lane);
-                row = xo;
-            },
-            [&](int run, const f32x4 (&acc)[G]) { finish((first + run * pitch) * kRows, lane & 15, acc); });
+        auto close = [&](int run, const f32x4 (&acc)[G]) { finish((first + run * pitch) * kRows, lane & 15, acc); };
+        if constexpr (NT)
+            stream<G, kUpDepth, kRows, NT>(0, (int64_t)mine * blocks, blocks, x, rings[wave], a.H, lane,
+                [&](int run, __amdgpu_buffer_rsrc_t (&w)[G], uint32_t (&wo)[2], uint32_t& row) {
+                    const int i0 = (first + run * pitch) * kRows;
+                    weights_of(i0, w);
+                    weight_offsets(wo, a.up_row, a.inner - i0, lane);
+                    row = xo;
+                }, close);
+        else
+            stream_lines<G, kUpDepth, kRows>(0, (int64_t)mine * blocks, blocks, a.up_row, x, rings[wave], a.H, lane,
+                [&](int run, int g) { return slice_weights(first + run * pitch, g); }, [&](int run) { return a.inner - (first + run * pitch) * kRows; },
+                [&](int) { return xo; }, close);
         return;
     }
     for (int slice = first; slice - wave / SPLIT < slices; slice += pitch) {
@@ -449,21 +568,30 @@ __global__ __launch_bounds__(64 * kDownWaves, 2) void layer_down_kernel(const La
     int most = 0;   // entries of one expert
     for (int i = lane; i < *table.count; i += 64) most = max(most, (int)table.start[i + 1] - (int)table.start[i]);
     if (!__any(most > 16)) {
-        stream<1, kDownDepth, ROWS, NT>(q, end, blocks, x, ring, a.inner, lane,
-            [&](int slot, __amdgpu_buffer_rsrc_t (&w)[1], uint32_t (&to)[2], uint32_t& row) {
-                to[0] = wo[0];
-                to[1] = wo[1];
-                const int e = __builtin_amdgcn_readfirstlane(table.expert[slot]), pos = table.start[slot] + (lane & 15);
-                w[0] = buffer(a.w_down + e * a.down_expert + (int64_t)h0 * a.down_row);
-                row = pos < table.start[slot + 1] ? (uint32_t)table.entry[pos] * (uint32_t)a.inner * 2 : kNowhere;
-            },
-            [&](int slot, const f32x4 (&acc)[1]) {
-                const int pos = table.start[slot] + (lane & 15);
-                if (pos < table.start[slot + 1] && (lane >> 4) * 4 < ROWS) {
-                    f32x4* to = (f32x4*)(mine + token_of(table.entry[pos]) * 16 + (lane >> 4) * 4);
-                    *to = *to + acc[0];
-                }
-            });
+        auto expert_of = [&](int slot) { return __builtin_amdgcn_readfirstlane(table.expert[slot]); };
+        auto row_of = [&](int slot) {
+            const int pos = table.start[slot] + (lane & 15);
+            return pos < table.start[slot + 1] ? (uint32_t)table.entry[pos] * (uint32_t)a.inner * 2 : kNowhere;
+        };
+        auto close = [&](int slot, const f32x4 (&acc)[1]) {
+            const int pos = table.start[slot] + (lane & 15);
+            if (pos < table.start[slot + 1] && (lane >> 4) * 4 < ROWS) {
+                f32x4* to = (f32x4*)(mine + token_of(table.entry[pos]) * 16 + (lane >> 4) * 4);
+                *to = *to + acc[0];
+            }
+        };
+        auto weights = [&](int slot, int) { return a.w_down + expert_of(slot) * a.down_expert + (int64_t)h0 * a.down_row; };
+        // eight columns: few workgroups, for which the time of one counts (344 columns 9.3 against 12.9 us by lines)
+        if constexpr (NT || ROWS == 8)
+            stream<1, kDownDepth, ROWS, NT>(q, end, blocks, x, ring, a.inner, lane,
+                [&](int slot, __amdgpu_buffer_rsrc_t (&w)[1], uint32_t (&to)[2], uint32_t& row) {
+                    to[0] = wo[0];
+                    to[1] = wo[1];
+                    w[0] = buffer(weights(slot, 0));
+                    row = row_of(slot);
+                }, close);
+        else
+            stream_lines<1, kDownDepth, ROWS>(q, end, blocks, a.down_row, x, ring, a.inner, lane, weights, [&](int) { return min(ROWS, a.H - h0); }, row_of, close);
         q = end;
     }
     while (q < end) {
