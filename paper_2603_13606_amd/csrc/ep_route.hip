@@ -317,8 +317,8 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_backward_kernel(const 
             d = g;
             if (a.renormalise) {
                 const float sum = wave_sum(s);
-                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-                d = (g - wave_sum(there ? g * s : 0.0f) * inv) * inv;
+                // from the weights, as above: of one entry, whose weight is 1 whatever its logit, exactly nothing is left
+                if (sum > 0.0f) d = (g - wave_sum(there ? g * (s / sum) : 0.0f)) / sum;
             }
             d = there ? d * s * rest : 0.0f;
         }

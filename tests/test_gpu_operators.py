@@ -156,6 +156,18 @@ def test_route_backward(ep, T, E, K, dtype, rule):
         assert out[:, E:].isnan().all()
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_one_renormalised_weight_has_no_gradient(ep, score):
+    """It is the scale whatever the logits are."""
+    l = torch.randn((70, 96), generator=gen_of(3), device=DEV)
+    rule = dict(score=getattr(ep, "EP_SCORE_" + score.upper()), scale=2.5)
+    idx, w, grad = torch.empty((70, 1), dtype=torch.int32, device=DEV), torch.empty((70, 1), device=DEV), torch.full((70, 96), POISON, device=DEV)
+    ep.ep_route(l, idx, w, **rule)
+    assert (w == 2.5).all()
+    ep.ep_route_backward(l, idx, torch.randn((70, 1), generator=gen_of(4), device=DEV), grad, **rule)
+    assert (grad == 0).all()
+
+
 # ---------------------------------------------------------------------- experts' products
 
 # rows per expert, Kd, output columns
