@@ -661,10 +661,13 @@ hipError_t launch_layer(const LayerArgs& a, hipStream_t s) {
     const int cus = compute_units();
     // Whole lines of weights: rows that start on lines.  A line that two blocks share would be fetched twice.
     auto lines = [](const void* p, int64_t expert, int64_t row) { return (uintptr_t)p % 128 == 0 && expert % 64 == 0 && row % 64 == 0; };
-    // up: two workgroups share a compute unit.  Where there are runs of rows for all their wavefronts, each takes runs of its
-    // own and no sums are joined; beyond twice as many it takes several, which spares the search for its expert's tokens.
+    // up: two workgroups share a compute unit.  Where there are runs of rows for half of their wavefronts, each takes runs of its
+    // own and no sums are joined (13 tokens of 40 experts, 2888 into 2 x 504: 34 us; with runs shared 47.8), for all of them
+    // where an expert has many tokens (64 of 8 experts, 2048 into 2 x 1024: 56.9 and 38.9); beyond that it takes several,
+    // which spares the search for its expert's tokens.
     const int slices = (a.inner + kRows - 1) / kRows;
-    const bool split = (int64_t)plan.slots * slices < 2 * kUpWaves * (int64_t)cus;
+    const bool many = a.T * a.K > 16 * plan.slots;
+    const bool split = (int64_t)plan.slots * slices < (many ? 2 : 1) * kUpWaves * (int64_t)cus;
     const int runs = split ? slices : (slices + kUpWaves - 1) / kUpWaves;
     plan.up_parts = std::clamp((4 * cus + plan.slots - 1) / plan.slots, 1, runs);
     // Where that leaves compute units idle, the tokens of an expert are shared out too: its weights then come from the L2
