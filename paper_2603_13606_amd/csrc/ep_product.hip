@@ -835,8 +835,8 @@ __device__ __forceinline__ int product(const Product& a, char* lds, Table* table
     // The tiles go in rounds of the workgroups.  Where the last round would leave half of them without a tile it takes halves
     // instead, whose steps take 5/8 of the time: all of them for small inputs, in one round (64 rows each of 48 experts, 1000
     // into 2888: 94 us in whole tiles, 83 so).  Where even tiles of 64 x 64 fit one round, those: 2 rows of 20 experts,
-    // 4704 into 944, take 45.5 us in halves and 18.1 so.  In two or three rounds they lose: 1158 rows of 3 experts, 336 into
-    // 2248, 12.6 and 17.7.
+    // 4704 into 944, take 45.5 us in halves and 18.1 so.  Or two rounds, where the contraction is long: 300 rows of one expert, 4096
+    // into 4096, 54 us in halves and 38 so, but 2000 rows of 16 experts, 1000 into 520, 17 and 19.
     Tiling t;
     t.columns = (a.I * (KIND == FORWARD && a.gated ? 2 : 1) + 255) / 256;
     t.blocks = KIND == GRAD_WEIGHTS ? whole_blocks(a.J, kBlockRows) : uniform(table->starts[a.win.L]);
@@ -853,14 +853,14 @@ __device__ __forceinline__ int product(const Product& a, char* lds, Table* table
     Tiling small = {(a.I * (KIND == FORWARD && a.gated ? 2 : 1) + kSmall - 1) / kSmall,
                     KIND == GRAD_WEIGHTS ? (a.J + kSmall - 1) / kSmall : uniform(table->smalls), 0, 0, 0};
     small.all = experts * small.blocks * small.columns;
-    if (small.all <= gridDim.x) {
+    if (small.all <= (KIND != GRAD_WEIGHTS && a.Kc >= 2048 ? 2 : 1) * (int64_t)gridDim.x) {
         if (KIND != GRAD_WEIGHTS) {
             if (threadIdx.x < 64) rescan_blocks(a.win.L, kSmall, table, threadIdx.x);
             __syncthreads();
         }
-        int64_t at = place(small.all);
+        int64_t at = small.all <= gridDim.x ? place(small.all) : (int64_t)(blockIdx.x & 7) * per + in;
         product_tiles<KIND, kSmall, kSmall>(a, lds, table, small, at, 0, small.all);
-        return (int)(small.all + 7) >> 3;
+        return ((int)(small.all + 7) >> 3) % per;
     }
     int64_t rest = t.all % gridDim.x;
     if (2 * rest > gridDim.x) rest = 0;

@@ -305,6 +305,7 @@ MANY = [
     (cycle([1, 128, 0, 17, 64, 65, 100], 140), 72, 120), (cycle([10, 200, 128, 129, 0, 300, 64], 140), 320, 200),
     (cycle([150, 131], 140), 40, 16), (cycle([160, 3], 90), 128, 264), (cycle([130, 20, 280], 40), 1600, 1000),
     (cycle([600, 90, 0], 12), 200, 2056), (cycle([3, 8], 1024), 64, 48),
+    (cycle([65, 1, 0, 190], 40), 2056, 264), (cycle([70, 30], 40), 264, 2056),   # two rounds of the smallest tiles, forward and backward
 ]
 
 
