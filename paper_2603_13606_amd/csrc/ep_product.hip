@@ -312,8 +312,8 @@ constexpr int kWaves = 8;            // wavefronts of a workgroup
 constexpr int kBlockRows = 256;      // rows per tile; short blocks: half
 constexpr int kFlatStages = 3;
 constexpr int kSmallStages = 4;      // of two steps each
-// Tiles of 256 x 256 in two stages, or half as large ones in three.
-constexpr int kLdsTiles = std::max(2 * (256 + 256) * kBK * 2, kFlatStages * (128 + 256) * kBK * 2);
+// Tiles of 256 x 256 in two stages, half as large ones in three, or those of 64 x 64 in four times two.
+constexpr int kLdsTiles = std::max({2 * (256 + 256) * kBK * 2, kFlatStages * (128 + 256) * kBK * 2, 2 * kSmallStages * (kSmall + kSmall) * kBK * 2});
 
 // What the tiles of a launch are: every one 256 along P (I); along Q (J) first the whole blocks, then the short ones.
 struct Tiling {
@@ -326,7 +326,7 @@ struct Tiling {
 //   256 x 256   tiles [t, end) of whole blocks in steps of the grid
 //   256 x 128   tiles [t, end) of short blocks (120 rows each of 32 experts, 7168 into 2 x 2048: 373 us in tiles of 256, 316 so)
 //   128 x 256   the halves of the tiles from `from` on, whatever their blocks
-//    64 x 64    tiles [t, end) of blocks of 64
+//    64 x 64    tiles [t, end) of blocks of 64, one or two per workgroup
 template <int KIND, int BI, int BJ>
 __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const Table* table, const Tiling& tiling, int64_t& t, int64_t from, int64_t end) {
     constexpr int NW = kWaves, NWI = BJ == 128 ? 4 : 2, NWJ = NW / NWI;   // wavefronts along P and along Q
