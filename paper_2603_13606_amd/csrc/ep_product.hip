@@ -456,7 +456,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     };
     if (!find()) return;
     begin(c);
-    int fresh = 1;   // no results have been stored since the tile's first loads
+    int fresh = 1;   // since the tile's first loads no results have been stored, or fewer than a full tile's
     for (;;) {
         const int steps = steps_of(c);
         const int Kc = KIND == GRAD_WEIGHTS ? c.rows : a.Kc;
@@ -704,6 +704,8 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
         const int iw = wi * (KIND == FORWARD && a.gated ? WI / 2 : WI), jw = wj * WJ + (mine & 15);
         const int i4 = iw + g * 4, i8 = iw + (g & 1) * 16 + (g >> 1) * 8;
         const int Il = a.I - done.i0;   // columns of the tile that there are
+        // Fragments of Q without a row: nothing to compute or to store (of a window with few rows most; the wide tile has few).
+        auto gone = [&](int jt) { return !WIDE && KIND != GRAD_WEIGHTS && wj * WJ + jt * 16 >= J; };
         const int esize = KIND == GRAD_WEIGHTS && a.out_f32 ? 4 : 2;
         // Byte offset of (index j of fragment jt, column i) in a matrix whose rows are `row` elements apart.
         auto at = [&](int jt, int i, int64_t row, int size) {
@@ -735,6 +737,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                 for (int it = 0; it < IT; it += SMALL ? 1 : 2)
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
+                        if (gone(jt)) continue;
                         const int i = (SMALL ? i4 : i8) + (it < nit ? it : it - nit) * 16;
                         const uint32_t to = at(jt, i, a.pre_row, 2) + (it < nit || i >= Il ? 0 : a.I * 2);
                         if constexpr (SMALL) store4(rp, to, acc[it][jt]);
@@ -748,6 +751,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                 for (int it = 0; it < kN; it += kH) {
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
+                        if (gone(jt)) continue;
                         f32x4 v[kH];
 #pragma unroll
                         for (int h = 0; h < kH; ++h)
@@ -796,6 +800,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                 for (int it = 0; it < IT; it += 2)
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
+                        if (gone(jt)) continue;
                         f32x4 v[2];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
@@ -824,7 +829,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             }
         }
         if (!again) return;
-        fresh = 0;
+        fresh = uniform(gone(JT - 1));   // fewer results stored than the waits count on
     }
 }
 
