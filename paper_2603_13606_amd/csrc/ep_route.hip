@@ -316,13 +316,15 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_backward_kernel(const 
         } else {
             s = there ? sigmoid_exact(le) : 0.0f;
             const float rest = there ? 1.0f / (1.0f + expf(le)) : 0.0f;  // 1 - s without cancellation
-            d = g;
+            d = there ? g * s * rest : 0.0f;
             if (a.renormalise) {
+                // From the weights, as above: the scores may be so small that the gradient of a weight over their sum overflows, where
+                // that of the logit does not.  Of one entry, whose weight is 1 whatever its logit, exactly nothing is left.
                 const float sum = wave_sum(s);
-                // from the weights, as above: of one entry, whose weight is 1 whatever its logit, exactly nothing is left
-                if (sum > 0.0f) d = (g - wave_sum(there ? g * (s / sum) : 0.0f)) / sum;
+                const float q = sum > 0.0f ? s / sum : 0.0f;
+                const float mean = wave_sum(there ? g * q : 0.0f);
+                d = there ? (g - mean) * q * rest : 0.0f;
             }
-            d = there ? d * s * rest : 0.0f;
         }
         float out[NPL];
 #pragma unroll

@@ -1,0 +1,80 @@
+"""The gate and the experts' operators at the limits of their ranges, on the GPU against 64-bit definitions."""
+import math
+
+import pytest
+import torch
+
+import operators_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def ep():
+    import ep_harness
+    ep_harness.ensure_built()
+    assert torch.cuda.is_available()
+    from paper_2603_13606_amd import binding
+    return binding
+
+
+def within(got, want, bound, what):
+    got, want, bound = got.double().cpu(), want.cpu(), bound.cpu()
+    bad = ~((got - want).abs() <= bound)
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()}, first at {bad.nonzero()[0].tolist()}: {got[bad][0]} for {want[bad][0]}"
+
+
+# ---------------------------------------------------------------------- gate: renormalised sigmoid scores near 0
+
+
+def faint_logits(E=24):
+    """Tokens whose selected scores are near the smallest float32 or below it; every entry names another expert."""
+    rows = [[-80.0, -80.0, -80.0, -80.0], [-88.5, -88.5, -88.25, -88.0], [-87.0, -88.7, -88.8, -95.0], [-6.0, -7.5, -6.5, -30.0],
+            [-9.0, -9.5, -60.0, -92.0], [-100.0, -100.0, -101.5, -100.25], [-300.0, -299.0, -300.0, -320.0], [-700.0, -701.0, -700.5, -707.0],
+            [3.0, -2.0, -90.0, 40.0], [-20.0, -20.0, -20.5, -21.0]]
+    l = torch.full((len(rows), E), -math.inf, device=DEV)
+    for t, r in enumerate(rows):
+        for k, v in enumerate(r):
+            l[t, (5 * k + 3 * t) % E] = v
+    return l
+
+
+def quotients(l, idx):
+    """Weights of the selected and 1 - score, in 64 bits."""
+    lk = torch.gather(l.double().cpu(), 1, idx.cpu().long())
+    return torch.softmax(torch.nn.functional.logsigmoid(lk), dim=1), torch.sigmoid(-lk)
+
+
+# Roundings: differences of logits of up to 100 (a step each of the exponent's argument), exponential, 1 + e, divisions, a sum of 4.
+STEPS = (100 + 24) * ref.U32
+# A score below the smallest normal float32 may be lost beside one of 2^-16 or more.
+LOST = 2.0 ** -110
+
+
+def gradient_of(p, rest, g, idx, shape):
+    """Gradient of the logits from p = w / scale and g = scale * gradient of w, and the sum of what it is made of."""
+    out, mag = (torch.zeros(shape, dtype=torch.float64) for _ in range(2))
+    at = idx.cpu().long()
+    out.scatter_add_(1, at, p * rest * (g - (g * p).sum(1, keepdim=True)))
+    mag.scatter_add_(1, at, p * rest * (g.abs() + (g * p).abs().sum(1, keepdim=True)))
+    return out, mag
+
+
+def check_gradient(ep, l, idx, size):
+    g = size * torch.tensor([1.0, -1.0, 2.0, -0.5], device=DEV).repeat(l.shape[0], 1)
+    grad = torch.full_like(l, math.nan)
+    ep.ep_route_backward(l, idx, g, grad, score=ep.EP_SCORE_SIGMOID, scale=2.5)
+    p, rest = quotients(l, idx)
+    want, mag = gradient_of(p, rest, 2.5 * g.double().cpu(), idx, l.shape)
+    within(grad, want, 2 * STEPS * mag + size * 16 * LOST, "grad_logits")
+
+
+@pytest.mark.parametrize("size", [1.0, 65536.0])
+def test_gradients_of_faint_scores_are_finite(ep, size):
+    """(g - mean) * score / sum, not (g - mean) / sum * score: with a loss scale in g the first quotient alone overflows."""
+    l = faint_logits()
+    l = l[(l.masked_fill(l == -math.inf, 0.0) >= -88.6).all(dim=1)].contiguous()
+    assert l.shape[0] == 4
+    check_gradient(ep, l, torch.stack([torch.nonzero(r > -math.inf).flatten() for r in l]).to(torch.int32), size)
