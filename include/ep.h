@@ -618,7 +618,8 @@ typedef struct {
  * there are no two; ties to the lower group).  Without bias and groups the order is that of the logits,
  * exactly; otherwise s + b is computed in 64 bits.  b takes part in the choice only:
  *     w[t,k] = scale * s[idx[t,k]] / (renormalise ? sum over the token's idx of s : 1)
- * in float32.  Entries that no routable expert is left for get id -1 and weight 0.
+ * in float32.  Renormalised sigmoid weights keep their meaning where the scores themselves leave the range of float32: only a
+ * score that leaves that of 64 bits too (a logit under -708.39) is 0.  Entries that no routable expert is left for get id -1 and weight 0.
  * Errors: EP_ERR_INVALID_ARG, EP_ERR_HIP.
  */
 EP_API ep_result_t ep_route(const ep_route_config_t *cfg, const ep_tensor_t *inputs, int32_t num_inputs,

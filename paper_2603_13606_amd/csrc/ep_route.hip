@@ -69,6 +69,14 @@ __device__ __forceinline__ float load_logit(const void* p, int64_t i, int is_bf1
 
 __device__ __forceinline__ float sigmoid_exact(float l) { return 1.0f / (1.0f + expf(-l)); }
 
+// Renormalised sigmoid scores relative to e^top, `top` the largest selected logit: for tokens whose scores add up to less than
+// kFaint, where single ones are lost below the range of float32 (logits under -87), or all of them.  Of at most 64 scores with a
+// larger sum the largest is 2^-16 or more, and what is lost beside it is less than 2^-110 of it.  As in 64 bits, a score below
+// 2^-1022 (a logit under -708.39) is 0.
+constexpr float kFaint = 0x1p-10f, kNoScore = -708.39f;
+static_assert(kMaxTopK <= 64, "scores that add up to kFaint");
+__device__ __forceinline__ float faint_score(float l, float top) { return l < kNoScore ? 0.0f : expf(l - top) / (1.0f + expf(l)); }
+
 // SCORES: selection by scores in 64 bits (bias or groups); otherwise by logits.
 template <int NPL, bool SCORES>
 __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs a) {
@@ -261,7 +269,12 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_kernel(const RouteArgs
             }
         }
         if (a.renormalise) {
-            const float sum = wave_sum(w);
+            float sum = wave_sum(w);
+            if (a.score == EP_SCORE_SIGMOID && sum < kFaint) {
+                const float most = unordered(wave_max(my_idx >= 0 ? ordered(my_l) : 0u));
+                w = my_idx >= 0 ? faint_score(my_l, most) : 0.0f;
+                sum = wave_sum(w);
+            }
             w = sum > 0.0f ? w / sum : 0.0f;
         }
         if (lane < a.K) {
@@ -320,8 +333,13 @@ __global__ __launch_bounds__(64 * kRouteWaves) void route_backward_kernel(const 
             if (a.renormalise) {
                 // From the weights, as above: the scores may be so small that the gradient of a weight over their sum overflows, where
                 // that of the logit does not.  Of one entry, whose weight is 1 whatever its logit, exactly nothing is left.
-                const float sum = wave_sum(s);
-                const float q = sum > 0.0f ? s / sum : 0.0f;
+                float q = s, sum = wave_sum(s);
+                if (sum < kFaint) {
+                    const float most = unordered(wave_max(there ? ordered(le) : 0u));
+                    q = there ? faint_score(le, most) : 0.0f;
+                    sum = wave_sum(q);
+                }
+                q = sum > 0.0f ? q / sum : 0.0f;
                 const float mean = wave_sum(there ? g * q : 0.0f);
                 d = there ? (g - mean) * q * rest : 0.0f;
             }

@@ -78,3 +78,30 @@ def test_gradients_of_faint_scores_are_finite(ep, size):
     l = l[(l.masked_fill(l == -math.inf, 0.0) >= -88.6).all(dim=1)].contiguous()
     assert l.shape[0] == 4
     check_gradient(ep, l, torch.stack([torch.nonzero(r > -math.inf).flatten() for r in l]).to(torch.int32), size)
+
+
+@pytest.mark.parametrize("bias,dtype", [(False, torch.float32), (True, torch.float32), (False, torch.bfloat16)])
+def test_faint_scores_keep_their_weights(ep, bias, dtype):
+    """Renormalised weights add up to the scale however small the scores are, and have gradients."""
+    l = faint_logits().to(dtype)
+    b = torch.zeros(l.shape[1], device=DEV) if bias else None
+    idx = torch.empty((l.shape[0], 4), dtype=torch.int32, device=DEV)
+    w = torch.empty((l.shape[0], 4), device=DEV)
+    ep.ep_route(l, idx, w, bias=b, score=ep.EP_SCORE_SIGMOID, scale=2.5)
+    assert all(sorted(i) == torch.nonzero(r > -math.inf).flatten().tolist() for i, r in zip(idx.tolist(), l))
+    if dtype == torch.float32:
+        p, _ = quotients(l, idx)
+        within(w, 2.5 * p, 2.5 * (STEPS * p + LOST), "weights")
+        for size in (1.0, 65536.0):
+            check_gradient(ep, l, idx, size)
+    assert torch.allclose(w.sum(1), torch.full_like(w[:, 0], 2.5), rtol=4 * ref.U32, atol=0)
+
+
+def test_scores_below_64_bits_are_zero(ep):
+    l = torch.tensor([[-708.3, -709.0, -800.0], [-709.0, -710.0, -3e38]], device=DEV)
+    idx, w = torch.empty((2, 2), dtype=torch.int32, device=DEV), torch.empty((2, 2), device=DEV)
+    ep.ep_route(l, idx, w, score=ep.EP_SCORE_SIGMOID)
+    assert idx.tolist() == [[0, 1], [0, 1]] and w.tolist() == [[1.0, 0.0], [0.0, 0.0]]
+    grad = torch.full_like(l, math.nan)
+    ep.ep_route_backward(l, idx, torch.tensor([[1.0, 2.0], [3.0, 4.0]], device=DEV), grad, score=ep.EP_SCORE_SIGMOID)
+    assert (grad == 0).all()
