@@ -177,14 +177,41 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
 
 __device__ __forceinline__ int spread(int k) { return ((k >> 1) & 1) | ((k >> 2) & 2); }
 
-// Sixteen bytes per lane from the buffer to LDS, lane after lane from the wave's address on.  Written in assembly, which
-// has no output register: the compiler puts a wait for all such loads in front of every transposing LDS read when it
-// knows of them, and would let none of them run ahead.  The waits are the caller's.
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, uint32_t offset, bool once = false) {
+// Loads of sixteen bytes per lane from the buffer to LDS, lane after lane from the wave's address `at` on, the next load's STEP bytes
+// behind.  Written in assembly, which has no output register: the compiler puts a wait for all such loads in front of every
+// transposing LDS read when it knows of them, and would let none of them run ahead.  The waits are the caller's.
+// A vector memory instruction may read an SGPR that a vector instruction has written (the descriptor's base, by readfirstlane)
+// five wait states later at the earliest; the compiler sees to that for instructions of its own, not for these.  s_mov and
+// s_nop 3 make up five, whatever stands in front; m0 itself needs one.  Once for all loads of a call: padded one by one they cost
+// the products 1 to 5 % (32768 rows of 8 experts, 7168 into 2 x 2048, 1403 against 1385 us; 128 rows of each, 112 against 106).
+// m0 is the compiler's own (it takes no word that an asm statement changes it), so nothing else in these kernels may use it.
+#define EP_FIRST "s_mov_b32 m0, %0\n\ts_nop 3\n\t"
+#define EP_NEXT "\n\ts_add_u32 m0, m0, %2\n\ts_nop 0\n\t"
+#define EP_LOAD(n, hint) "buffer_load_dwordx4 %" #n ", %1, 0 offen " hint "lds"
+#define EP_LOADS1(hint) EP_FIRST EP_LOAD(3, hint)
+#define EP_LOADS2(hint) EP_LOADS1(hint) EP_NEXT EP_LOAD(4, hint)
+#define EP_LOADS4(hint) EP_LOADS2(hint) EP_NEXT EP_LOAD(5, hint) EP_NEXT EP_LOAD(6, hint)
+template <int STEP, int N>
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, const uint32_t (&off)[N], bool once) {
+    static_assert(N == 1 || N == 2 || N == 4, "");
     const uint32_t at = (uint32_t)(uintptr_t)(lds_ptr)lds;
-    if (once) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(at), "v"(offset), "s"(rsrc) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(rsrc) : "memory");
+    if constexpr (N == 1) {
+        if (once) asm volatile(EP_LOADS1("nt ") ::"s"(at), "s"(rsrc), "n"(STEP), "v"(off[0]) : "memory");
+        else asm volatile(EP_LOADS1("") ::"s"(at), "s"(rsrc), "n"(STEP), "v"(off[0]) : "memory");
+    } else if constexpr (N == 2) {
+        if (once) asm volatile(EP_LOADS2("nt ") ::"s"(at), "s"(rsrc), "n"(STEP), "v"(off[0]), "v"(off[1]) : "memory", "scc");
+        else asm volatile(EP_LOADS2("") ::"s"(at), "s"(rsrc), "n"(STEP), "v"(off[0]), "v"(off[1]) : "memory", "scc");
+    } else {
+        if (once) asm volatile(EP_LOADS4("nt ") ::"s"(at), "s"(rsrc), "n"(STEP), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory", "scc");
+        else asm volatile(EP_LOADS4("") ::"s"(at), "s"(rsrc), "n"(STEP), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory", "scc");
+    }
 }
+#undef EP_FIRST
+#undef EP_NEXT
+#undef EP_LOAD
+#undef EP_LOADS1
+#undef EP_LOADS2
+#undef EP_LOADS4
 
 template <int B, bool KM, int NW, bool HINT>
 struct Operand {
@@ -229,12 +256,13 @@ struct Operand {
     __device__ __forceinline__ void load(char* lds, int left, int wave) {
         const auto rsrc = buffer(base);
         const bool hint = HINT && uniform(once);
+        uint32_t o[J1 - J0];
 #pragma unroll
         for (int j = J0; j < J1; ++j) {
             const int k = KM ? k0 : k0 + ((j * NW + wave) & 7) * 8;
-            const uint32_t o = k < left ? off[j] : kNowhere;
-            load_to_lds(rsrc, lds + (j * NW + wave) * 1024, o, hint);
+            o[j - J0] = k < left ? off[j] : kNowhere;
         }
+        load_to_lds<NW * 1024>(rsrc, lds + (J0 * NW + wave) * 1024, o, hint);
     }
     __device__ __forceinline__ void next() { base += step; }
 };
