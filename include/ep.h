@@ -446,7 +446,8 @@ EP_API ep_result_t ep_handle_get_num_recv_tokens(ep_handle_t handle, int64_t *nu
  * for everything queued there; a later ep_layout on the same stream is ordered by the stream.
  * What the caller must see to: calls of one handle on several streams must have been ordered
  * among themselves so that the last call's stream comes after the others (as data dependencies
- * between dispatch and combine require anyway).  A staged call that was never completed is
+ * between dispatch and combine require anyway; an expert product of the weights' gradients, whose
+ * results no later call of the handle needs, is one of them too).  A staged call that was never completed is
  * abandoned: its coordination counters are cleared on the stream of its send phase. */
 EP_API ep_result_t ep_handle_destroy(ep_handle_t handle);
 

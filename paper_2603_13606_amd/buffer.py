@@ -35,6 +35,7 @@ class EPHandle:
         self.topk_idx = topk_idx
         self.num_tokens = num_tokens
         self.alive = True
+        self.products = {}  # stream -> event behind the last expert product there (they read the handle's row counts)
 
 
 class EPBuffer:
@@ -259,7 +260,9 @@ class EPBuffer:
         return grad_y, grad_w, self._leave(compute, run, capturing, grad_y, grad_w)
 
     # ------------------------------------------------------------------ the gate and the experts
-    # Computation, not communication: these run on the compute stream, whatever stream dispatch and combine take.
+    # Computation, not communication: these run on the compute stream, whatever stream dispatch and combine take, and no call
+    # waits for them that was not told to.  What the products read of the handle stays theirs until they have ended: `destroy_handle`
+    # waits for them.  (For replays of a graph that holds products the caller waits.)
 
     def route(self, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, score: str = "softmax", renormalise: bool = True,
               num_groups: int = 1, groups_kept: int = 1, scale: float = 1.0) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -275,8 +278,7 @@ class EPBuffer:
         N = weights.shape[1]
         out = torch.empty((*x.shape[:-1], N // 2 if gated else N), dtype=torch.bfloat16, device=x.device)
         pre = torch.empty((*x.shape[:-1], N), dtype=torch.bfloat16, device=x.device) if keep_pre else None
-        with self._lock:
-            self._behind_calls()
+        with self._product(handle):
             ep.ep_expert_product(x, weights, out, handle=handle.raw, bias=bias, residual=residual, pre=pre, activation=_ACTS[activation],
                                  gated=gated, first_expert=first_expert)
         return out, pre
@@ -293,8 +295,7 @@ class EPBuffer:
         shape = (weights if weights is not None else grad_weights).shape
         grad_pre = torch.empty_like(pre) if pre is not None else None
         grad_x = torch.zeros((*grad_out.shape[:-1], shape[2]), dtype=torch.bfloat16, device=grad_out.device) if weights is not None else None
-        with self._lock:
-            self._behind_calls()
+        with self._product(handle):
             ep.ep_expert_product_backward(grad_out, weights, handle=handle.raw, x=x, pre=pre, grad_pre=grad_pre, grad_x=grad_x,
                                           grad_weights=grad_weights, grad_bias=grad_bias, activation=_ACTS[activation], gated=gated,
                                           first_expert=first_expert, accumulate=accumulate)
@@ -307,11 +308,22 @@ class EPBuffer:
         without dispatch and combine."""
         return expert_layer(x, topk_idx, topk_weights, w_up, w_down, bias_up, bias_down, residual, activation, gated, first_expert)
 
-    def _behind_calls(self) -> None:
-        """The compute stream waits for the calls made so far, if it has not yet (the windows' row counts are read there)."""
-        compute = torch.cuda.current_stream()
-        if self._order_event is not None and compute.cuda_stream not in self._order_streams and not torch.cuda.is_current_stream_capturing():
-            compute.wait_event(self._order_event)
+    @contextlib.contextmanager
+    def _product(self, handle: EPHandle):
+        """Around a product: the compute stream waits for the calls made so far, if it has not yet (the windows' row counts are read
+        there), and the handle keeps the event behind the product."""
+        with self._lock:
+            compute = torch.cuda.current_stream()
+            capturing = torch.cuda.is_current_stream_capturing()
+            if self._order_event is not None and compute.cuda_stream not in self._order_streams and not capturing:
+                compute.wait_event(self._order_event)
+            try:
+                yield
+            finally:
+                if not capturing:
+                    ev = torch.cuda.Event()
+                    ev.record(compute)
+                    handle.products[compute.cuda_stream] = ev
 
     def get_tokens_per_expert_list(self) -> List[int]:
         """Rows placed per expert by the last dispatch, read from the pinned counter."""
@@ -335,10 +347,12 @@ class EPBuffer:
         return ep.ep_handle_get_num_recv_tokens(handle.raw)
 
     def destroy_handle(self, handle: EPHandle) -> None:
-        """Deferred destruction (Sec. VI-B): wait for the last recorded event, then release."""
+        """Deferred destruction (Sec. VI-B): wait for the last recorded event and for the handle's products, then release."""
         if handle.alive:
             if self._last_event is not None:
                 self._last_event.synchronize()
+            for ev in handle.products.values():
+                ev.synchronize()
             ep.ep_handle_destroy(handle.raw)
             handle.alive = False
 

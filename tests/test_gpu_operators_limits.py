@@ -105,3 +105,39 @@ def test_scores_below_64_bits_are_zero(ep):
     grad = torch.full_like(l, math.nan)
     ep.ep_route_backward(l, idx, torch.tensor([[1.0, 2.0], [3.0, 4.0]], device=DEV), grad, score=ep.EP_SCORE_SIGMOID)
     assert (grad == 0).all()
+
+
+# ---------------------------------------------------------------------- the buffer's products and the life of a handle
+
+
+def test_a_handle_outlives_a_product_that_is_held_back(ep):
+    """Weight gradients queued behind other work on a side stream; meanwhile the handle is combined with, destroyed, and its place
+    taken by the next routing, all on the communication stream: the product still sees its own windows."""
+    from paper_2603_13606_amd import buffer as B
+    T, E, H, K, N = 64, 8, 128, 2, 40
+    gen = torch.Generator(DEV)
+    gen.manual_seed(3)
+    normal = lambda *s: torch.randn(s, generator=gen, device=DEV).bfloat16()  # noqa: E731
+    x, y, g = normal(T, H), normal(T * K, H), normal(T * K, N)
+    one = torch.stack([torch.arange(T) % 3, 3 + torch.arange(T) % 5], 1).to(torch.int32).to(DEV)
+    two = torch.full((T, K), 7, dtype=torch.int32, device=DEV)
+    two[:, 0] = 6
+    buf = B.EPBuffer(2, E, H, K, max_tokens_per_rank=T, max_handles=1)
+    try:
+        recv, _, _, h, _ = buf.dispatch(x, one)
+        want, got = (torch.full((E, N, H), math.nan, device=DEV) for _ in range(2))
+        buf.expert_product_backward(g, h, x=recv, grad_weights=want)
+        torch.cuda.synchronize()
+        ev = buf.capture()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+            buf.expert_product_backward(g, h, x=recv, grad_weights=got)
+        buf.combine(y, h, previous_event=ev)
+        buf.destroy_handle(h)
+        _, _, _, other, _ = buf.dispatch(x, two, previous_event=ev)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.isfinite(want).all()
+        buf.destroy_handle(other)
+    finally:
+        buf.close()
