@@ -127,8 +127,7 @@ class EPBuffer:
         capturing = torch.cuda.is_current_stream_capturing()
         comm = self._comm
         sp = compute.cuda_stream
-        if (previous_event is None and not self._comm_given and not capturing and compute.device_index == comm.device_index
-                and (sp == 0 or compute.stream_id != sp)):
+        if previous_event is None and not self._comm_given and not capturing and compute.device_index == comm.device_index and self._lasts(compute):
             run = compute
         else:
             run, sp = comm, comm.cuda_stream
@@ -139,6 +138,11 @@ class EPBuffer:
         if not capturing and self._order_event is not None and sp not in self._order_streams:
             run.wait_event(self._order_event)
         return compute, run, capturing
+
+    @staticmethod
+    def _lasts(stream: torch.cuda.Stream) -> bool:
+        """Whether torch made the stream: another's owner may destroy it while the library still remembers it."""
+        return stream.cuda_stream == 0 or stream.stream_id != stream.cuda_stream
 
     def _on(self, compute: torch.cuda.Stream, run: torch.cuda.Stream):
         return contextlib.nullcontext() if run is compute else torch.cuda.stream(run)
@@ -278,9 +282,9 @@ class EPBuffer:
         N = weights.shape[1]
         out = torch.empty((*x.shape[:-1], N // 2 if gated else N), dtype=torch.bfloat16, device=x.device)
         pre = torch.empty((*x.shape[:-1], N), dtype=torch.bfloat16, device=x.device) if keep_pre else None
-        with self._product(handle):
+        with self._product(handle) as run:
             ep.ep_expert_product(x, weights, out, handle=handle.raw, bias=bias, residual=residual, pre=pre, activation=_ACTS[activation],
-                                 gated=gated, first_expert=first_expert)
+                                 gated=gated, first_expert=first_expert, stream=run)
         return out, pre
 
     def expert_product_backward(self, grad_out: torch.Tensor, handle: EPHandle, weights: Optional[torch.Tensor] = None,
@@ -295,10 +299,10 @@ class EPBuffer:
         shape = (weights if weights is not None else grad_weights).shape
         grad_pre = torch.empty_like(pre) if pre is not None else None
         grad_x = torch.zeros((*grad_out.shape[:-1], shape[2]), dtype=torch.bfloat16, device=grad_out.device) if weights is not None else None
-        with self._product(handle):
+        with self._product(handle) as run:
             ep.ep_expert_product_backward(grad_out, weights, handle=handle.raw, x=x, pre=pre, grad_pre=grad_pre, grad_x=grad_x,
                                           grad_weights=grad_weights, grad_bias=grad_bias, activation=_ACTS[activation], gated=gated,
-                                          first_expert=first_expert, accumulate=accumulate)
+                                          first_expert=first_expert, accumulate=accumulate, stream=run)
         return grad_x, grad_pre
 
     def expert_layer(self, x: torch.Tensor, topk_idx: torch.Tensor, topk_weights: Optional[torch.Tensor], w_up: torch.Tensor,
@@ -310,20 +314,27 @@ class EPBuffer:
 
     @contextlib.contextmanager
     def _product(self, handle: EPHandle):
-        """Around a product: the compute stream waits for the calls made so far, if it has not yet (the windows' row counts are read
-        there), and the handle keeps the event behind the product."""
+        """Around a product, which gets the stream to run on: the compute stream, behind the calls made so far (the windows' row
+        counts are read there); the handle keeps the event behind the product.  Where the compute stream is one that torch did
+        not make, which the library must not remember (see `_start`), the communication stream takes the product's place in it."""
         with self._lock:
             compute = torch.cuda.current_stream()
             capturing = torch.cuda.is_current_stream_capturing()
-            if self._order_event is not None and compute.cuda_stream not in self._order_streams and not capturing:
-                compute.wait_event(self._order_event)
+            run = compute if self._lasts(compute) else self._comm
+            if run is not compute:
+                run.wait_stream(compute)
+            if self._order_event is not None and run.cuda_stream not in self._order_streams and not capturing:
+                run.wait_event(self._order_event)
             try:
-                yield
+                yield run
             finally:
-                if not capturing:
+                if run is not compute or not capturing:
                     ev = torch.cuda.Event()
-                    ev.record(compute)
-                    handle.products[compute.cuda_stream] = ev
+                    ev.record(run)
+                    if run is not compute:
+                        compute.wait_event(ev)
+                    if not capturing:
+                        handle.products[run.cuda_stream] = ev
 
     def get_tokens_per_expert_list(self) -> List[int]:
         """Rows placed per expert by the last dispatch, read from the pinned counter."""

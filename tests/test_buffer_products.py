@@ -107,3 +107,16 @@ def test_products_under_capture_leave_no_event(buf):
     buf.compute.capturing = False
     buf.destroy_handle(buf.handle)
     assert waited == ["destroyed"]
+
+
+@pytest.mark.parametrize("call", [forward, backward])
+@pytest.mark.parametrize("capturing", [False, True])
+def test_a_stream_of_somebody_else_is_not_remembered(buf, call, capturing):
+    """Its owner may destroy it while the handle lives: the product runs on the communication stream, in its place."""
+    theirs = Stream(7, torchs=False)
+    theirs.capturing = capturing
+    with torch.cuda.stream(theirs):
+        call(buf)
+    assert [e if isinstance(e, str) else e[0] for e in buf._comm.log] == ["waits for stream", "product", "event"]
+    assert buf._comm.log[0][1] == 7 and theirs.log == [("waits for", buf._comm.log[-1][1])]
+    assert list(buf.handle.products) == ([] if capturing else [2])

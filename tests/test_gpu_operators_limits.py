@@ -141,3 +141,36 @@ def test_a_handle_outlives_a_product_that_is_held_back(ep):
         buf.destroy_handle(other)
     finally:
         buf.close()
+
+
+def test_products_on_a_stream_of_somebody_else(ep):
+    """The same results on a stream that torch did not make, behind what is queued there and before what follows."""
+    from paper_2603_13606_amd import buffer as B
+    T, E, H, K, N = 50, 8, 64, 2, 24
+    gen = torch.Generator(DEV)
+    gen.manual_seed(5)
+    normal = lambda *s: torch.randn(s, generator=gen, device=DEV).bfloat16()  # noqa: E731
+    idx = torch.randint(0, E, (T, K), generator=gen, device=DEV, dtype=torch.int32)
+    x, w, g = normal(T, H), normal(E, N, H), normal(T * K, N)
+    owner = torch.cuda.Stream()
+    theirs = torch.cuda.ExternalStream(owner.cuda_stream)
+    buf = B.EPBuffer(2, E, H, K, max_tokens_per_rank=T)
+    try:
+        recv, _, _, h, _ = buf.dispatch(x, idx)
+        rows = buf.get_num_recv_tokens(h)
+        want, _ = buf.expert_product(recv, w, h)
+        want_gx, _ = buf.expert_product_backward(g, h, w)
+        torch.cuda.synchronize()
+        late = torch.zeros_like(recv)
+        with torch.cuda.stream(theirs):
+            torch.cuda._sleep(2_000_000)
+            late.copy_(recv)
+            out, _ = buf.expert_product(late, w, h)
+            out = out.clone()
+            gx, _ = buf.expert_product_backward(g, h, w)
+            gx = gx.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:rows], want[:rows]) and torch.equal(gx, want_gx)
+        buf.destroy_handle(h)
+    finally:
+        buf.close()
