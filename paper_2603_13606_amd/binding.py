@@ -618,10 +618,13 @@ class PreparedOperator:
 
 
 def _one_device(tensors) -> Optional[int]:
-    """The library launches on the current device: a tensor of another one is the caller's mistake.  Returns the device."""
+    """The library launches on the current device: a tensor of another one, or one in the host's memory among those of a GPU, is the
+    caller's mistake (pinned memory can be read by the GPU).  Returns the device."""
     gpu = {t.device for t in tensors if t.is_cuda}
     if len(gpu) > 1 or (gpu and next(iter(gpu)).index != torch.cuda.current_device()):
         raise ValueError(f"tensors on {sorted(map(str, gpu))}, current device cuda:{torch.cuda.current_device()}")
+    if gpu and any(not t.is_cuda and t.numel() and not t.is_pinned() for t in tensors):
+        raise ValueError(f"tensors on {sorted({str(t.device) for t in tensors})}: those in the host's memory are out of the GPU's reach")
     return next(iter(gpu)).index if gpu else None
 
 
