@@ -317,6 +317,8 @@ class EPBuffer:
         """Around a product, which gets the stream to run on: the compute stream, behind the calls made so far (the windows' row
         counts are read there); the handle keeps the event behind the product.  Where the compute stream is one that torch did
         not make, which the library must not remember (see `_start`), the communication stream takes the product's place in it."""
+        if not handle.alive:
+            raise ValueError("the handle has been destroyed")
         with self._lock:
             compute = torch.cuda.current_stream()
             capturing = torch.cuda.is_current_stream_capturing()

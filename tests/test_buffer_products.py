@@ -120,3 +120,12 @@ def test_a_stream_of_somebody_else_is_not_remembered(buf, call, capturing):
     assert [e if isinstance(e, str) else e[0] for e in buf._comm.log] == ["waits for stream", "product", "event"]
     assert buf._comm.log[0][1] == 7 and theirs.log == [("waits for", buf._comm.log[-1][1])]
     assert list(buf.handle.products) == ([] if capturing else [2])
+
+
+@pytest.mark.parametrize("call", [forward, backward])
+def test_products_of_a_destroyed_handle_are_refused(buf, call):
+    """As in a backward pass that comes too late: the library has freed what the handle points to."""
+    buf.destroy_handle(buf.handle)
+    with pytest.raises(ValueError):
+        call(buf)
+    assert "product" not in buf.compute.log
