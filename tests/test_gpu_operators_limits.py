@@ -174,3 +174,40 @@ def test_products_on_a_stream_of_somebody_else(ep):
         buf.destroy_handle(h)
     finally:
         buf.close()
+
+
+# ---------------------------------------------------------------------- gelu far below 0
+
+
+def gelu_inputs():
+    """Every bf16 number from -13 to -1/64, and some above."""
+    v = torch.arange(0x3c80, 0x4151, device=DEV).to(torch.int16).view(torch.bfloat16)
+    return torch.cat([-v, torch.linspace(0, 12, 96, device=DEV).bfloat16()])[:-((v.numel() + 96) % 8) or None].reshape(-1, 8).contiguous()
+
+
+# Of the value: half a step of bf16, and 2^-15 for what float32 and the part's exponential do to arguments of up to 85.
+GELU = ref.BF16 + 2.0 ** -15
+
+
+@pytest.mark.parametrize("gated", [False, True])
+def test_gelu_is_as_exact_far_below_zero(ep, gated):
+    v = gelu_inputs()
+    n = v.shape[0]
+    eye = torch.eye(8, device=DEV, dtype=torch.bfloat16)[None]
+    off, cnt = torch.zeros(1, dtype=torch.int32, device=DEV), torch.full((1,), n, dtype=torch.int32, device=DEV)
+    out = torch.full_like(v, math.nan)
+    if gated:   # the up projection is 1: its weights are 0, its bias 1
+        w, b = torch.cat([eye, torch.zeros_like(eye)], 1), torch.tensor([[0.0] * 8 + [1.0] * 8], device=DEV)
+    else:
+        w, b = eye, None
+    ep.ep_expert_product(v, w, out, bias=b, row_offset=off, row_count=cnt, activation=ep.EP_ACT_GELU, gated=gated)
+    want = ref.act("gelu", v.double())
+    within(out, want, GELU * want.abs() + ref.TINY, "gelu")
+    pre = torch.cat([v, torch.ones_like(v)], 1) if gated else v
+    grad = torch.full_like(pre, math.nan)
+    ep.ep_expert_product_backward(torch.ones_like(v), w, pre=pre, grad_pre=grad, grad_x=torch.empty_like(v), row_offset=off, row_count=cnt,
+                                  activation=ep.EP_ACT_GELU, gated=gated)
+    d, cdf = ref.act_grad("gelu", v.double()), ref.act("gelu", v.double()) / v.double().where(v != 0, 1.0)
+    within(grad[:, :8], d, ref.BF16 * d.abs() + 2.0 ** -15 * (cdf.abs() + (d - cdf).abs()) + ref.TINY, "its derivative")
+    if gated:
+        within(grad[:, 8:], want, GELU * want.abs() + ref.TINY, "gelu in the backward pass")
