@@ -666,7 +666,7 @@ typedef struct {
  * windows are left untouched.  Rows of a window beyond the shortest row tensor are skipped and, with a
  * handle, flagged (status bit 2).  r may be out itself.
  * N (and N/2), Kd multiples of 8; every row on a 16-byte boundary, rows less than 2^22 elements apart, the
- * rows of an output apart from each other;
+ * rows of an output apart from each other; at most 2^31 - 256 rows in a 2-D tensor or in a window of a 3-D one;
  * a gated expert's weights span less than 2^31 bytes (else EP_ERR_UNSUPPORTED).  One expert is a plain
  * matrix product with bias, activation and residual.
  * Errors: EP_ERR_INVALID_ARG, EP_ERR_UNSUPPORTED, EP_ERR_HIP.

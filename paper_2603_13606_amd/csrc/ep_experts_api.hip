@@ -12,6 +12,7 @@ using namespace ep;
 namespace {
 
 constexpr int64_t kMaxExtent = 1 << 22;      // rows' lengths and strides, elements: a tile's offsets stay below 2^31 bytes
+constexpr int64_t kMaxRows = 0x7fffff00LL;   // of a window or a tensor: rounded up to blocks of 256 they are counted in 32 bits
 constexpr int64_t kMaxLayerExtent = 1 << 17; // of the layer: its grid stays below 2^32 work-items
 constexpr int64_t kMaxLayerRows = 1 << 30;   // elements between the layer's products: 32-bit byte offsets
 constexpr int kMaxGroups = 64;
@@ -108,7 +109,7 @@ ep_result_t find_windows(ep_handle_t h, const ep_product_config_t* cfg, const ep
         r->win.offset = off ? (const int32_t*)off->data : nullptr;
         r->win.count = (const int32_t*)cnt->data;
     }
-    r->win.cap = r->padded ? r->slots : 0x7fffffffLL;
+    r->win.cap = r->padded ? r->slots : kMaxRows;
     return EP_SUCCESS;
 }
 
@@ -120,13 +121,13 @@ bool row_tensor(const ep_tensor_t* t, int64_t cols, Rows* r, RowsDesc* d, bool w
     const int64_t row = t->stride[inner - 1];
     if (row < cols || row % 8 || row >= kMaxExtent) return false;
     if (r->padded) {
-        if (t->shape[0] != r->tensor_experts || t->shape[1] != r->slots || t->shape[1] < 0 || t->shape[1] > 0x7fffffffLL) return false;
+        if (t->shape[0] != r->tensor_experts || t->shape[1] != r->slots || t->shape[1] < 0 || t->shape[1] > kMaxRows) return false;
         if (t->stride[0] < 0 || t->stride[0] % 8) return false;
         if ((!t->data && t->shape[1] > 0) || (written && !apart(t))) return false;
         d->expert_stride = t->stride[0];
         d->base = (uint16_t*)t->data + r->first * t->stride[0];
     } else {
-        if (t->shape[0] < 0 || t->shape[0] > 0x7fffffffLL || (!t->data && t->shape[0] > 0)) return false;
+        if (t->shape[0] < 0 || t->shape[0] > kMaxRows || (!t->data && t->shape[0] > 0)) return false;
         d->expert_stride = 0;
         d->base = (uint16_t*)t->data;
         r->win.cap = std::min(r->win.cap, t->shape[0]);

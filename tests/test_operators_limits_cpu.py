@@ -31,3 +31,24 @@ def test_tensors_in_host_memory_among_those_of_a_gpu_are_refused(ep, monkeypatch
     pinned = type("Pinned", (), dict(is_cuda=False, device=torch.device("cpu"), numel=lambda self: 4, is_pinned=lambda self: True))()
     assert ep._one_device([OnGpu(), empty, pinned]) == 0
     assert ep._one_device([host, empty]) is None
+
+
+@pytest.mark.parametrize("padded", [False, True])
+def test_more_rows_than_blocks_can_count_are_refused(ep, padded):
+    """Rounded up to blocks of 256 rows their number has to stay below 2^31.  (The descriptors are all there is: nothing of that
+    size is allocated, and a call that passed the checks would fail for want of a GPU.)"""
+    if torch.cuda.is_available():
+        pytest.skip("the call would be made")
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)    # noqa: E731
+    rows = bf(1, 4, 8) if padded else bf(4, 8)
+    ins = [(rows, ep.EP_TAG_TOKENS), (bf(1, 8, 8), ep.EP_TAG_EXPERT_WEIGHTS), (i32(1), ep.EP_TAG_ROW_COUNT)] + [(i32(1), ep.EP_TAG_ROW_OFFSET)] * (not padded)
+    cfg = ep._product_config(ep.EP_ACT_NONE, False)
+
+    def call(n):
+        x, out = (ep.tensor_desc(rows, ep.EP_TAG_TOKENS) for _ in range(2))
+        x.shape[int(padded)] = out.shape[int(padded)] = n
+        descs = (ep.ep_tensor_t * len(ins))(x, *[ep.tensor_desc(t, tag) for t, tag in ins[1:]])
+        return ep.load().ep_expert_product(None, ctypes.byref(cfg), descs, len(ins), (ep.ep_tensor_t * 1)(out), 1, None)
+    assert call(2 ** 31 - 1) == call(2 ** 31 - 255) == ep.EP_ERR_INVALID_ARG
+    assert call(2 ** 31 - 256) != ep.EP_ERR_INVALID_ARG
