@@ -31,7 +31,7 @@ ep_result_t check_route(const ep_route_config_t* cfg, const ep_tensor_t* logits,
     if (!std::isfinite(cfg->scale)) return EP_ERR_INVALID_ARG;
     if (!logits || logits->ndim != 2 || !float_or_bf16(logits) || !idx || idx->ndim != 2) return EP_ERR_INVALID_ARG;
     const int64_t T = logits->shape[0], E = logits->shape[1], K = idx->shape[1];
-    if (E < 1 || E > kMaxExperts || K < 1 || K > kMaxTopK || T < 0 || T * K > (1 << 28)) return EP_ERR_INVALID_ARG;
+    if (E < 1 || E > kMaxExperts || K < 1 || K > kMaxTopK || T < 0 || T > (1 << 28) / K) return EP_ERR_INVALID_ARG;
     if (!check_rows(logits, logits->dtype, E) || !check_2d(idx, EP_DTYPE_I32, T, K, true) || !check_2d(w, EP_DTYPE_F32, T, K, true))
         return EP_ERR_INVALID_ARG;
     if (cfg->num_groups < 1 || cfg->num_groups > kMaxGroups || E % cfg->num_groups || cfg->groups_kept < 1 ||

@@ -52,3 +52,18 @@ def test_more_rows_than_blocks_can_count_are_refused(ep, padded):
         return ep.load().ep_expert_product(None, ctypes.byref(cfg), descs, len(ins), (ep.ep_tensor_t * 1)(out), 1, None)
     assert call(2 ** 31 - 1) == call(2 ** 31 - 255) == ep.EP_ERR_INVALID_ARG
     assert call(2 ** 31 - 256) != ep.EP_ERR_INVALID_ARG
+
+
+def test_numbers_of_tokens_that_overflow_are_refused(ep):
+    """2^61 tokens of 8 entries are 2^64, which is 0 in 64 bits; the call seemed to have worked."""
+    ls, idx, w = torch.zeros(4, 16), torch.zeros((4, 8), dtype=torch.int32), torch.zeros(4, 8)
+
+    def desc(t, tag, n):
+        d = ep.tensor_desc(t, tag)
+        d.shape[0] = n
+        return d
+    for n in (2 ** 61, 2 ** 25 + 1):
+        l, i, g = desc(ls, ep.EP_TAG_LOGITS, n), desc(idx, ep.EP_TAG_TOPK_IDX, n), desc(w, ep.EP_TAG_TOPK_WEIGHTS, n)
+        cfg, lib, arr = ep._route_config(ep.EP_SCORE_SOFTMAX, True, 1, 1, 1.0), ep.load(), ep.ep_tensor_t
+        assert lib.ep_route(ctypes.byref(cfg), (arr * 1)(l), 1, (arr * 2)(i, g), 2, None) == ep.EP_ERR_INVALID_ARG
+        assert lib.ep_route_backward(ctypes.byref(cfg), (arr * 3)(l, i, g), 3, (arr * 1)(l), 1, None) == ep.EP_ERR_INVALID_ARG
