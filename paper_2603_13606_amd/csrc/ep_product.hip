@@ -870,13 +870,7 @@ __device__ __forceinline__ int product(const Product& a, char* lds, Table* table
     // into 2888: 94 us in whole tiles, 83 so).  Where even tiles of 64 x 64 fit one round, those: 2 rows of 20 experts,
     // 4704 into 944, take 45.5 us in halves and 18.1 so.  Or two rounds, where the contraction is long: 300 rows of one expert, 4096
     // into 4096, 54 us in halves and 38 so, but 2000 rows of 16 experts, 1000 into 520, 17 and 19.
-    Tiling t;
-    t.columns = (a.I * (KIND == FORWARD && a.gated ? 2 : 1) + 255) / 256;
-    t.blocks = KIND == GRAD_WEIGHTS ? whole_blocks(a.J, kBlockRows) : uniform(table->starts[a.win.L]);
-    t.shorts = KIND == GRAD_WEIGHTS ? short_blocks(a.J, kBlockRows) : uniform(table->shorts[a.win.L]);
     const int64_t experts = KIND == GRAD_WEIGHTS ? a.win.L : 1;
-    t.whole = experts * t.blocks * t.columns;
-    t.all = t.whole + experts * t.shorts * t.columns;
     const int per = gridDim.x >> 3;
     // The place of this workgroup in a round of n tiles, as many on each XCD and neighbours together; n where it has none.
     auto place = [&](int64_t n) {
@@ -887,7 +881,7 @@ __device__ __forceinline__ int product(const Product& a, char* lds, Table* table
                     KIND == GRAD_WEIGHTS ? (a.J + kSmall - 1) / kSmall : uniform(table->smalls), 0, 0, 0};
     small.all = experts * small.blocks * small.columns;
     if (small.all <= (KIND != GRAD_WEIGHTS && a.Kc >= 2048 ? 2 : 1) * (int64_t)gridDim.x) {
-        if (KIND != GRAD_WEIGHTS) {
+        if (KIND != GRAD_WEIGHTS) {   // whose entries nobody has read yet
             if (threadIdx.x < 64) rescan_blocks(a.win.L, kSmall, table, threadIdx.x);
             __syncthreads();
         }
@@ -895,6 +889,12 @@ __device__ __forceinline__ int product(const Product& a, char* lds, Table* table
         product_tiles<KIND, kSmall, kSmall>(a, lds, table, small, at, 0, small.all);
         return ((int)(small.all + 7) >> 3) % per;
     }
+    Tiling t;
+    t.columns = (a.I * (KIND == FORWARD && a.gated ? 2 : 1) + 255) / 256;
+    t.blocks = KIND == GRAD_WEIGHTS ? whole_blocks(a.J, kBlockRows) : uniform(table->starts[a.win.L]);
+    t.shorts = KIND == GRAD_WEIGHTS ? short_blocks(a.J, kBlockRows) : uniform(table->shorts[a.win.L]);
+    t.whole = experts * t.blocks * t.columns;
+    t.all = t.whole + experts * t.shorts * t.columns;
     int64_t rest = t.all % gridDim.x;
     if (2 * rest > gridDim.x) rest = 0;
     const int64_t mine = (int64_t)(blockIdx.x & 7) * per + in;
