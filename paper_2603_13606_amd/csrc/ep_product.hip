@@ -183,7 +183,7 @@ __device__ __forceinline__ int spread(int k) { return ((k >> 1) & 1) | ((k >> 2)
 // A vector memory instruction may read an SGPR that a vector instruction has written (the descriptor's base, by readfirstlane)
 // five wait states later at the earliest; the compiler sees to that for instructions of its own, not for these.  s_mov and
 // s_nop 3 make up five, whatever stands in front; m0 itself needs one.  Once for all loads of a call: padded one by one they cost
-// the products 1 to 5 % (32768 rows of 8 experts, 7168 into 2 x 2048, 1403 against 1385 us; 128 rows of each, 112 against 106).
+// the products 1 to 5 % (32768 rows of 8 experts, 7168 into 2 x 2048: 1403 against 1385 us).
 // m0 is the compiler's own (it takes no word that an asm statement changes it), so nothing else in these kernels may use it.
 #define EP_FIRST "s_mov_b32 m0, %0\n\ts_nop 3\n\t"
 #define EP_NEXT "\n\ts_add_u32 m0, m0, %2\n\ts_nop 0\n\t"
@@ -367,6 +367,11 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
     using Q = Operand<BJ, kQK, NW, false>;
     constexpr int kStage = P::kBytes + Q::kBytes;
     constexpr int kLoads = P::kLoads + Q::kLoads;
+    // Results: a store takes kPair fragments of P for one of Q.  A tile issues at least kStores of them per lane, whether a lane has
+    // something there or not, and half as many where a gate takes half of the accumulators; the waits for loads that were issued
+    // before them count on that.
+    constexpr int kPair = SMALL ? 1 : 2, kStores = IT / kPair * JT, kGatedStores = IT / 2 / kPair * JT;
+    static_assert(IT % (2 * kPair) == 0, "whole stores, gated ones too");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wi = wave % NWI, wj = wave / NWI;
 
@@ -536,18 +541,17 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             // k + 2 and two in phase 0 of step k + 1, and in both places waiting for all but the youngest eight leaves
             // what the next phase reads in LDS.
             static_assert(P::kLoads == 4 && Q::kLoads == 4 && NW == 8, "");
-            constexpr int IH = IT / 2;
+            constexpr int IH = IT / 2, kAhead = 1 + 1 + Q::kLoads;   // loads for step 1 that begin() issues
             if (steps) {
-                // Step 0 has landed when only the six loads for step 1 and the results stored since are on their way: of
-                // those at least 8 (gated) or 16 per lane.
+                // Step 0 has landed when only those for step 1 and the results stored since are on their way.
                 if (steps == 1) {
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 } else if (uniform(fresh)) {
-                    asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
                 } else if (KIND == FORWARD && a.gated) {
-                    asm volatile("s_waitcnt vmcnt(14)" ::: "memory");
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead + kGatedStores) : "memory");
                 } else {
-                    asm volatile("s_waitcnt vmcnt(22)" ::: "memory");
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead + kStores) : "memory");
                 }
                 barrier();
                 if (late) barrier();
@@ -662,10 +666,10 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             // product interval (32 instructions, as long) per step, and three stages: the loads of step k + 2 take the place
             // of step k - 1, which everybody has read.
             if (steps) {
-                // besides step 1's loads the results stored since may be on their way: at least 4 (gated) or 8 per lane
+                // besides step 1's loads the results stored since may be on their way
                 if (steps == 1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 else if (uniform(fresh)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-                else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads + (KIND == FORWARD ? IT * JT / 4 : IT * JT / 2)) : "memory");
+                else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads + (KIND == FORWARD ? kGatedStores : kStores)) : "memory");
                 barrier();
                 if (late) barrier();
             }
@@ -762,7 +766,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             if (a.pre) {
                 const auto rp = buffer(a.pre + done.e * a.pre_expert + (done.first + done.j0) * a.pre_row + done.i0);
 #pragma unroll
-                for (int it = 0; it < IT; it += SMALL ? 1 : 2)
+                for (int it = 0; it < IT; it += kPair)
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
                         if (gone(jt)) continue;
@@ -774,15 +778,15 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
             }
             const auto rr = buffer(a.res + done.e * a.res_expert + (done.first + done.j0) * a.res_row + done.i0);
             auto finish = [&](auto activation, auto gate) {
-                constexpr int kN = decltype(gate)::value ? IT / 2 : IT, kH = SMALL ? 1 : 2;
+                constexpr int kN = decltype(gate)::value ? IT / 2 : IT;
 #pragma unroll
-                for (int it = 0; it < kN; it += kH) {
+                for (int it = 0; it < kN; it += kPair) {
 #pragma unroll
                     for (int jt = 0; jt < JT; ++jt) {
                         if (gone(jt)) continue;
-                        f32x4 v[kH];
+                        f32x4 v[kPair];
 #pragma unroll
-                        for (int h = 0; h < kH; ++h)
+                        for (int h = 0; h < kPair; ++h)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 v[h][r] = activate(decltype(activation)::value, acc[it + h][jt][r]);
@@ -791,7 +795,7 @@ __device__ __forceinline__ void product_tiles(const Product& a, char* lds, const
                         if (a.res) {
                             if constexpr (WIDE) {
 #pragma unroll
-                                for (int h = 0; h < kH; ++h) v[h] += load4(rr, at(jt, i4 + (it + h) * 16, a.res_row, 2), 0);
+                                for (int h = 0; h < kPair; ++h) v[h] += load4(rr, at(jt, i4 + (it + h) * 16, a.res_row, 2), 0);
                             } else if constexpr (SMALL) v[0] += widen(res[it][jt]);
                             else add8(res[it / 2 % kResidual][jt], v[0], v[1]);
                         }
