@@ -107,6 +107,49 @@ def test_scores_below_64_bits_are_zero(ep):
     assert (grad == 0).all()
 
 
+# ---------------------------------------------------------------------- gate: more tokens than wavefronts of a launch
+
+
+def many_tokens(dtype, E=16, T=70001):
+    gen = torch.Generator(DEV)
+    gen.manual_seed(11)
+    l = torch.randn((T, E), generator=gen, device=DEV) * 2
+    l[torch.rand((T, E), generator=gen, device=DEV) < 0.2] = -math.inf
+    return gen, l.to(dtype)
+
+
+@pytest.mark.parametrize("groups,kept", [(1, 1), (4, 2)])
+def test_route_many_tokens(ep, groups, kept):
+    """Wavefronts take several tokens each: everything of the first one, group keys included, gives way to the next."""
+    _, l = many_tokens(torch.float32)
+    (T, E), K = l.shape, 3
+    idx, w = torch.full((T, K), -7, dtype=torch.int32, device=DEV), torch.full((T, K), math.nan, device=DEV)
+    ep.ep_route(l, idx, w, renormalise=False, num_groups=groups, groups_kept=kept, scale=1.5)
+    s, _, there = ref.route_scores(l.double().cpu(), "softmax")
+    key = torch.where(there, s, -math.inf)
+    if groups > 1:
+        two = key.view(T, groups, -1).topk(2, dim=2).values
+        worth = two[:, :, 0] + two[:, :, 1].clamp(min=0.0)
+        best = worth.sort(dim=1, descending=True, stable=True).indices[:, :kept]
+        key = key.masked_fill(~torch.zeros(T, groups, dtype=torch.bool).scatter(1, best, True).repeat_interleave(E // groups, 1), -math.inf)
+    top, order = key.sort(dim=1, descending=True, stable=True)
+    some = top[:, :K] > -math.inf
+    assert torch.equal(idx.cpu(), torch.where(some, order[:, :K], -1).to(torch.int32))
+    want = torch.where(some, 1.5 * s.gather(1, order[:, :K]), 0.0)
+    within(w, want, (20 + E + 16) * ref.U32 * want + ref.TINY, "weights")
+
+
+@pytest.mark.parametrize("dtype,score,renormalise", [(torch.float32, "softmax", False), (torch.bfloat16, "sigmoid", True)])
+def test_route_backward_many_tokens(ep, dtype, score, renormalise):
+    gen, l = many_tokens(dtype)
+    (T, E), K = l.shape, 3
+    idx = torch.randint(-1, E, (T, K), generator=gen, device=DEV, dtype=torch.int32)
+    g = torch.randn((T, K), generator=gen, device=DEV)
+    grad = torch.full_like(l, math.nan)
+    ep.ep_route_backward(l, idx, g, grad, score=getattr(ep, "EP_SCORE_" + score.upper()), renormalise=renormalise)
+    within(grad, *ref.route_grad(l, idx, g, score, renormalise), "grad_logits")
+
+
 # ---------------------------------------------------------------------- the buffer's products and the life of a handle
 
 
