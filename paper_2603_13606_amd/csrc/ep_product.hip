@@ -933,7 +933,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void gradients_kernel(const Product
     product<GRAD_WEIGHTS>(w, lds, table, in >= used ? in - used : in - used + per);
 }
 
-// grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows: 16384 rows of 2 x 1408 in 49 us, 4.7 TB/s.
+// grad_pre = grad_out * d out / d pre, a workgroup per block of 16 rows: 16384 rows of 2 x 1408 in 49 us, 4.7 TB/s.  It is rounded
+// to bf16 once, as the gradient that the caller gets, and the products read that: their errors then are those of two roundings
+// (2.3e-3 against the 1.7e-3 of one).  A second bf16 part for them would double the matrix instructions that bound them.
 constexpr int kActRows = 16;
 
 __device__ __forceinline__ void unpack8(const uint4& u, float (&f)[8]) {
