@@ -612,8 +612,9 @@ typedef struct {
  * ep_combine take them.
  * inputs:  LOGITS l [T, E] f32 or bf16, any row stride (E <= 1024); SELECT_BIAS b f32 [E] (optional).
  * outputs: TOPK_IDX int32 [T, K] (K <= 64, T * K <= 2^28); TOPK_WEIGHTS f32 [T, K].
- * s = softmax(l) over the token's routable experts, or sigmoid(l).  An expert is not routable where its
- * logit is -inf or NaN (or its bias is); +inf counts as the largest finite float.  The K routable experts
+ * s = softmax(l) over the experts of the token that are there, or sigmoid(l).  An expert is not there where its logit is -inf or
+ * NaN; +inf counts as the largest finite float.  It is routable if its bias is neither -inf nor NaN either (which takes it out of the
+ * choice, not out of the softmax: b has no part in s).  The K routable experts
  * with the largest s + b are taken in descending order, ties to the lower id; with groups only experts of
  * the groups_kept groups with the largest sum of their two largest s + b (of the one routable member, if
  * there are no two; ties to the lower group).  Without bias and groups the order is that of the logits,

@@ -150,6 +150,27 @@ def test_route_backward_many_tokens(ep, dtype, score, renormalise):
     within(grad, *ref.route_grad(l, idx, g, score, renormalise), "grad_logits")
 
 
+def test_a_bias_takes_experts_out_of_the_choice_only(ep):
+    """The scores are those of the logits: plain softmax weights count the experts that the bias keeps from being chosen, as the
+    backward pass does, which knows no bias."""
+    l = torch.tensor([[0.5, 2.0, 1.0, -1.0, 0.0, -math.inf, 0.25, 1.5]], device=DEV)
+    b = torch.tensor([0.0, math.nan, -math.inf, 1.0, 0.0, 0.0, 0.0, 2.0], device=DEV)
+    idx, w = torch.empty((1, 8), dtype=torch.int32, device=DEV), torch.empty((1, 8), device=DEV)
+    ep.ep_route(l, idx, w, bias=b, renormalise=False)
+    assert idx.tolist() == [[7, 3, 0, 6, 4, -1, -1, -1]]
+    leaf = l.double().cpu().requires_grad_(True)
+    s = torch.softmax(leaf, dim=1)
+    want = torch.cat([s[:, [7, 3, 0, 6, 4]], torch.zeros(1, 3)], dim=1)
+    within(w, want.detach(), 40 * ref.U32 * want.detach(), "weights")
+    g = torch.tensor([[1.0, -2.0, 0.5, 3.0, -1.0, 7.0, 7.0, 7.0]], device=DEV)
+    (want * g.double().cpu()).sum().backward()
+    grad = torch.full_like(l, math.nan)
+    ep.ep_route_backward(l, idx, g, grad, renormalise=False)
+    assert grad[0, 5] == 0
+    there = [0, 1, 2, 3, 4, 6, 7]
+    within(grad[:, there], leaf.grad[:, there], torch.full((1, 7), 8 * 60 * ref.U32, dtype=torch.float64), "grad_logits")
+
+
 # ---------------------------------------------------------------------- the buffer's products and the life of a handle
 
 
