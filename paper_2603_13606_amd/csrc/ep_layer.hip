@@ -16,7 +16,7 @@
 //         dimension) pairs evenly, each adds up its own part of the output for all tokens in LDS, and the
 //         parts are joined in wave order.  No atomics on values: results do not depend on timing.
 // Measured: one token of 64 experts, top-8, 7168 and 2 x 2048: up 72 us (6.5 TB/s), down 43 (5.4, 448 workgroups on 256
-// compute units); 128 tokens of 128 experts, 4096 and 2 x 1408, every expert named: 468 and 231 (6.3).
+// compute units); 128 tokens of 128 experts, 4096 and 2 x 1408, every expert named: 495 and 242 (6.0), one behind the other 702 (6.3).
 // An expert works on its own tokens only, so what its weights hold (an infinity, a NaN) reaches no others.
 #include <algorithm>
 

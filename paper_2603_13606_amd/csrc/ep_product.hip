@@ -11,8 +11,8 @@
 // in memory is read from LDS 16 bytes per lane; one whose contraction index is the row (the weights of
 // grad_x, both operands of grad_W) goes through the transposing LDS read.
 //
-// Measured: forward, 32768 rows of 8 experts, 7168 into 2 x 2048: 1.41 PFLOP/s, matrix units busy 85 % at the 1.6 GHz that
-// the power limit leaves; both gradients of 16384 rows of 8, 4096 and 2 x 1408: 1.16 PFLOP/s, 63 % at 1.9 GHz; 128 rows
+// Measured: forward, 32768 rows of 8 experts, 7168 into 2 x 2048: 1.37 to 1.42 PFLOP/s, matrix units busy 82 to 85 % at the
+// 1.6 GHz that the power limit leaves; both gradients of 16384 rows of 8, 4096 and 2 x 1408: 1.13 PFLOP/s, 61 % at 1.9 GHz; 128 rows
 // each of 8, 7168 into 2 x 2048: 95 us, of which reading the weights takes 69.
 #include <algorithm>
 #include <atomic>
@@ -183,7 +183,7 @@ __device__ __forceinline__ int spread(int k) { return ((k >> 1) & 1) | ((k >> 2)
 // A vector memory instruction may read an SGPR that a vector instruction has written (the descriptor's base, by readfirstlane)
 // five wait states later at the earliest; the compiler sees to that for instructions of its own, not for these.  s_mov and
 // s_nop 3 make up five, whatever stands in front; m0 itself needs one.  Once for all loads of a call: padded one by one they cost
-// the products 1 to 5 % (32768 rows of 8 experts, 7168 into 2 x 2048: 1403 against 1385 us).
+// the products 1 to 5 % (32768 rows of 8 experts, 7168 into 2 x 2048: 1403 against 1385 us); one statement for both operands, 1 to 2 %.
 // m0 is the compiler's own (it takes no word that an asm statement changes it), so nothing else in these kernels may use it.
 #define EP_FIRST "s_mov_b32 m0, %0\n\ts_nop 3\n\t"
 #define EP_NEXT "\n\ts_add_u32 m0, m0, %2\n\ts_nop 0\n\t"
